@@ -142,6 +142,7 @@ typedef struct sale_params {
 /* sale_sparse_attn without parking slots (see there); one slot more per SALE_PARKED_ROW_BYTES. */
 #define SALE_WS_SPARSE_ATTN_MIN 7
 #define SALE_PARKED_ROW_BYTES 33792u
+#define SALE_WS_PROMPT_ATTN 8
 
 /* Bytes of workspace `which_call` needs for `p` (0 if the call needs none or the
  * parameters are invalid). */
@@ -337,6 +338,97 @@ int sale_calibrate_tau(const sale_params_t* p, const void* q, const void* k, con
                        float tau0, float theta, int32_t max_halvings,
                        float* tau_out, float* err_out, int32_t* halvings_out,
                        void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Serving: prompts of any length, a cache of pages, single-token attention.
+ * ---------------------------------------------------------------------------
+ * The calls below read batch, n_q_heads, n_kv_heads, seq_len, head_dim (128), the strides, n_seqs and cu_seqlens of
+ * sale_params_t; its blocks (block_q .. local_blocks) are not read and flags must be 0.  seq_len is ANY positive number
+ * here, and so are the lengths of packed sequences (n_seqs > 0: batch = 1; ascending offsets, two of which may be equal: a
+ * sequence of no tokens).  Q, K, V, O and pages are 16-byte aligned (SALE_ERR_BAD_SHAPE).
+ */
+
+/*
+ * Causal attention over whole prompts (Eq. 1 with M = M_c) of any lengths: sale_dense_attn without its multiples of 64.
+ * Nothing is padded by the caller; no token outside the sequences is read or written.  Sequences of up to 262144 tokens.
+ *   o, lse : as at sale_dense_attn (lse with the accuracy stated at sale_sparse_attn)
+ *   ws     : workspace of sale_workspace_bytes(p, SALE_WS_PROMPT_ATTN) bytes
+ */
+int sale_prompt_attn(const sale_params_t* p, const void* q, const void* k, const void* v,
+                     void* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Element type of the pages of a cache. */
+#define SALE_PAGE_BF16 0
+#define SALE_PAGE_FP8 1 /* OCP E4M3: key = value * k_scale[KV head], the same for values */
+
+/*
+ * Keys and values of many sequences in pages of page_tokens tokens.  The program owns all of it and decides which page
+ * belongs to whom; the calls read the structure itself during the call and everything it points to on the stream.
+ *   element (page, KV head h, token slot, c) of K lies at  k + page * k_stride[0] + h * k_stride[1] + slot * k_stride[2] + c
+ * (all-zero strides: contiguous [page][n_kv_heads][page_tokens][head_dim]); strides are non-negative multiples of 16 bytes,
+ * the token stride head_dim .. 2^24 elements; V likewise.
+ *   table : int32 [sequences][table_width], the pages of each sequence in order: position i of sequence s is slot
+ *           i % page_tokens of page table[s][i / page_tokens].  An entry outside 0 .. n_pages - 1 is no page: its positions
+ *           hold no keys and what is appended there is dropped.
+ *   lens  : int32 [sequences], tokens that a sequence holds; negative counts as 0.  Positions from table_width * page_tokens
+ *           on hold no keys, whatever lens says
+ * Table and lens are device memory and may change from call to call (or replay to replay of a captured graph).
+ */
+typedef struct sale_cache {
+  void* k;
+  void* v;
+  const float* k_scale; /* SALE_PAGE_FP8: fp32 [n_kv_heads] (device), positive; otherwise not read */
+  const float* v_scale;
+  int64_t k_stride[3];  /* element strides of (page, KV head, token) */
+  int64_t v_stride[3];
+  int32_t n_pages;
+  int32_t page_tokens;  /* 16, 32, 64, 128 or 256 */
+  int32_t dtype;        /* SALE_PAGE_* */
+  int32_t table_width;
+  const int32_t* table;
+  const int32_t* lens;
+} sale_cache_t;
+
+/*
+ * Writes the keys and values of new tokens into the cache.  With n the number of new tokens of sequence s (seq_len, or the
+ * length of packed sequence s), token i of them goes to position lens[s] - n + i: lens already counts the new tokens.
+ * Tokens whose position is negative, lies beyond the table or in no page are dropped.  Nothing else of the pages is
+ * written.  Where two sequences of a call write the same slot of a page, one of the two values is left there.
+ *   k, v in : bf16, strided as everywhere.  SALE_PAGE_FP8 keeps e4m3(x / scale[h]): IEEE fp32 division, limited to +-448,
+ *             round to nearest even, NaN stays NaN.
+ */
+int sale_cache_append(const sale_params_t* p, const sale_cache_t* cache, const void* k, const void* v, void* stream);
+
+/*
+ * Copies whole pages, K and V: page dst[i] becomes page src[i], i = 0 .. n - 1.  What a fork of a sequence (its last, partly
+ * filled page) and a compaction move; the rest of both, and freeing, is the program's list of pages.
+ *   src, dst in : HOST arrays, read during the call.  Pages 0 .. n_pages - 1, the dst all different and none of them
+ *                 among the src (SALE_ERR_BAD_SHAPE); a page may be copied to several.  n = 0 does nothing.
+ * Reads n_kv_heads and head_dim of p; table and lens of the cache may be NULL.
+ */
+int sale_cache_copy(const sale_params_t* p, const sale_cache_t* cache, const int32_t* src, const int32_t* dst, int32_t n,
+                    void* stream);
+
+/*
+ * Attention of the last seq_len tokens of every sequence (one when generating, more when drafted tokens are checked) to the
+ * cache.  All sequences share a prefix of prefix_len keys, whose pages are prefix_table and which are read once for all
+ * of them; a sequence's own keys, its new tokens among them (append first), follow it.  Query t of sequence s sees the
+ * prefix and the own positions 0 .. lens[s] - seq_len + t.  O = softmax(Q K^T / sqrt(d)) V over these, probabilities
+ * rounded to bf16 before the product with V and summed in fp32 before rounding.  A query that sees no key (an empty slot of
+ * the batch) gets O = 0 and lse = -inf.  Keys that a query does not see have no effect, whatever is in their place.
+ *   p            : batch = sequences; n_q_heads / n_kv_heads * seq_len at most 64; n_seqs = 0
+ *   q        in  : bf16, strided;  o out: bf16, strided
+ *   prefix_table in : int32 [ceil(prefix_len / page_tokens)] (device), entries as in the table; NULL if prefix_len = 0
+ *   lse      out : optional fp32 [batch][n_q_heads][seq_len], natural log of the sum
+ *   ws           : workspace of sale_decode_workspace_bytes(p, cache, prefix_len) bytes (0: none needed)
+ * How the keys are split over workgroups follows from the sizes given here, not from lens, so a captured call serves every
+ * lens; results do not depend on what else runs.
+ */
+int sale_decode_attn(const sale_params_t* p, const sale_cache_t* cache, const void* q,
+                     const int32_t* prefix_table, int32_t prefix_len,
+                     void* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+size_t sale_decode_workspace_bytes(const sale_params_t* p, const sale_cache_t* cache, int32_t prefix_len);
 
 #ifdef __cplusplus
 }

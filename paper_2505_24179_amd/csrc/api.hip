@@ -3,6 +3,25 @@
 
 namespace sale {
 
+namespace {
+
+// strides: all zero (contiguous) or non-negative multiples of 8 elements with whole rows apart
+int validate_strides(const sale_params_t* p) {
+  const int64_t* triples[4] = {p->q_stride, p->k_stride, p->v_stride, p->o_stride};
+  const int heads_of[4] = {p->n_q_heads, p->n_kv_heads, p->n_kv_heads, p->n_q_heads};
+  for (int x = 0; x < 4; ++x) {
+    const int64_t* st = triples[x];
+    if (st[0] == 0 && st[1] == 0 && st[2] == 0) continue;
+    for (int e = 0; e < 3; ++e)
+      if (st[e] < 0 || (st[e] & 7)) return SALE_ERR_BAD_SHAPE;
+    if (st[2] < p->head_dim) return SALE_ERR_BAD_SHAPE;
+    if ((heads_of[x] > 1 && st[1] == 0) || (p->batch > 1 && st[0] == 0)) return SALE_ERR_BAD_SHAPE;
+  }
+  return SALE_OK;
+}
+
+}  // namespace
+
 int validate_common(const sale_params_t* p, GeomClass cls) {
   if (p->batch <= 0 || p->n_q_heads <= 0 || p->n_kv_heads <= 0 || p->seq_len <= 0) return SALE_ERR_BAD_SHAPE;
   if (p->block_q <= 0 || p->block_k <= 0) return SALE_ERR_BAD_SHAPE;
@@ -31,20 +50,32 @@ int validate_common(const sale_params_t* p, GeomClass cls) {
     if (p->block_q != kBlockQ) return SALE_ERR_UNSUPPORTED;
     if (longest / p->block_k > kMaskWordsMax * 64) return SALE_ERR_UNSUPPORTED;
   }
-  // strides: all zero (contiguous) or non-negative multiples of 8 elements with whole rows apart
-  const int64_t* triples[4] = {p->q_stride, p->k_stride, p->v_stride, p->o_stride};
-  const int heads_of[4] = {p->n_q_heads, p->n_kv_heads, p->n_kv_heads, p->n_q_heads};
-  for (int x = 0; x < 4; ++x) {
-    const int64_t* st = triples[x];
-    if (st[0] == 0 && st[1] == 0 && st[2] == 0) continue;
-    for (int e = 0; e < 3; ++e)
-      if (st[e] < 0 || (st[e] & 7)) return SALE_ERR_BAD_SHAPE;
-    if (st[2] < p->head_dim) return SALE_ERR_BAD_SHAPE;
-    if ((heads_of[x] > 1 && st[1] == 0) || (p->batch > 1 && st[0] == 0)) return SALE_ERR_BAD_SHAPE;
-  }
+  const int rc = validate_strides(p);
+  if (rc != SALE_OK) return rc;
   // 32-bit index guards used by the kernels
   if ((long)p->batch * p->n_q_heads * (long)(p->seq_len / 32) > 0x7FFFFFFFL) return SALE_ERR_UNSUPPORTED;
   return SALE_OK;
+}
+
+int validate_tokens(const sale_params_t* p) {
+  if (p->batch <= 0 || p->n_q_heads <= 0 || p->n_kv_heads <= 0 || p->seq_len <= 0) return SALE_ERR_BAD_SHAPE;
+  if (p->n_q_heads % p->n_kv_heads != 0) return SALE_ERR_BAD_SHAPE;
+  if (p->head_dim != kHeadDim || p->flags != 0) return SALE_ERR_UNSUPPORTED;
+  if (p->n_seqs < 0 || (p->n_seqs > 0 && !p->cu_seqlens)) return SALE_ERR_BAD_SHAPE;
+  if (p->n_seqs > 0) {
+    if (p->batch != 1 || p->cu_seqlens[0] != 0 || p->cu_seqlens[p->n_seqs] != p->seq_len) return SALE_ERR_BAD_SHAPE;
+    for (int s = 0; s < p->n_seqs; ++s)
+      if (p->cu_seqlens[s + 1] < p->cu_seqlens[s]) return SALE_ERR_BAD_SHAPE;
+  }
+  return validate_strides(p);
+}
+
+Strided layout_of(const int64_t* stride, int heads, int seq_len) {
+  if (stride[0] == 0 && stride[1] == 0 && stride[2] == 0) {
+    const long long sh = (long long)seq_len * kHeadDim;
+    return {sh * heads, sh, kHeadDim, heads};
+  }
+  return {stride[0], stride[1], stride[2], heads};
 }
 
 int longest_sequence(const sale_params_t* p) {
@@ -66,24 +97,16 @@ Geo make_geo(const sale_params_t* p) {
   g.n_kb = p->seq_len / p->block_k;
   g.words = (longest_sequence(p) / p->block_k + 63) / 64;
   g.seq_start = nullptr;
+  g.tokens_of = nullptr;
+  g.tokens = p->seq_len;
   g.sink_blocks = p->sink_blocks;
   g.local_blocks = p->local_blocks;
   g.seg = (p->flags & SALE_FLAG_SEGMENT_LOCAL) ? kSegmentBlocks : 0;
   g.stats_causal = (p->flags & SALE_FLAG_STATS_CAUSAL) ? 1 : 0;
-  auto layout = [&](const int64_t* st, int heads) {
-    Strided s;
-    s.heads = heads;
-    if (st[0] == 0 && st[1] == 0 && st[2] == 0) {
-      s.st = kHeadDim; s.sh = (long long)p->seq_len * kHeadDim; s.sb = s.sh * heads;
-    } else {
-      s.sb = st[0]; s.sh = st[1]; s.st = st[2];
-    }
-    return s;
-  };
-  g.sq = layout(p->q_stride, p->n_q_heads);
-  g.sk = layout(p->k_stride, p->n_kv_heads);
-  g.sv = layout(p->v_stride, p->n_kv_heads);
-  g.so = layout(p->o_stride, p->n_q_heads);
+  g.sq = layout_of(p->q_stride, p->n_q_heads, p->seq_len);
+  g.sk = layout_of(p->k_stride, p->n_kv_heads, p->seq_len);
+  g.sv = layout_of(p->v_stride, p->n_kv_heads, p->seq_len);
+  g.so = layout_of(p->o_stride, p->n_q_heads, p->seq_len);
   return g;
 }
 
@@ -131,7 +154,9 @@ int build_seq_table(const sale_params_t* p, int32_t* table, hipStream_t st) {
 using namespace sale;
 
 extern "C" size_t sale_workspace_bytes(const sale_params_t* p, int which_call) {
-  if (!p || validate_common(p, kGeomPath) != SALE_OK) return 0;
+  if (!p) return 0;
+  if (which_call == SALE_WS_PROMPT_ATTN) return prompt_workspace_bytes(p);
+  if (validate_common(p, kGeomPath) != SALE_OK) return 0;
   const size_t rows = (size_t)p->batch * p->n_q_heads * p->seq_len;
   switch (which_call) {
     case SALE_WS_SELECT:

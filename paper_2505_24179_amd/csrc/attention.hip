@@ -128,7 +128,9 @@ struct OrderJob {
 // Without the copy of K the first pass over the 8-bit operands follows in the same launch, from workgroup `tiles` on.
 struct Then8 { int tiles; Pass8 pass; };
 struct NoPass8 {};
-template <bool K, bool V>
+// ODD: sequences of any length (Geo::tokens_of).  Behind a sequence's last token V' is zero and K' repeats its last key (which
+// only queries behind it would see).
+template <bool K, bool V, bool ODD = false>
 __global__ __launch_bounds__(256) void rearrange_kv_kernel(Geo g, OrderJob job, std::conditional_t<K, NoPass8, Then8> then,
                                                            const uint16_t* __restrict__ k,
                                                            const uint16_t* __restrict__ v,
@@ -149,13 +151,15 @@ __global__ __launch_bounds__(256) void rearrange_kv_kernel(Geo g, OrderJob job, 
   if (slot_counter && block == 0 && tid == 0) *slot_counter = 0;      // (for order_units_kernel, next on the stream)
   const size_t tile = block;                           // flattened (kv head, block j): rows tile*64 .. +63
   const int tiles_per_head = seq / 64;
-  const uint16_t* kt = k + row_off(lk, (int)(tile / tiles_per_head), (int)(tile % tiles_per_head) * 64);
-  const uint16_t* vt = v + row_off(lv, (int)(tile / tiles_per_head), (int)(tile % tiles_per_head) * 64);
+  const int2 part = ODD ? g.tokens_of[tile % tiles_per_head] : make_int2((int)(tile % tiles_per_head) * 64, 64);
+  const uint16_t* kt = k + row_off(lk, (int)(tile / tiles_per_head), part.x);
+  const uint16_t* vt = v + row_off(lv, (int)(tile / tiles_per_head), part.x);
 #pragma unroll
   for (int r = 0; r < (V ? 4 : 0); ++r) {
     const int chunk = tid + 256 * r;                   // V tile -> LDS, rows padded by one bank
     const int row = chunk >> 4, col = (chunk & 15) * 8;
-    const u32x4 w = *(const u32x4*)(vt + (size_t)row * lv.st + col);
+    u32x4 w = {0, 0, 0, 0};
+    if (!ODD || row < part.y) w = *(const u32x4*)(vt + (size_t)row * lv.st + col);
     uint32_t* d = (uint32_t*)&sv[row * (kHeadDim + 2) + col];
     d[0] = w[0]; d[1] = w[1]; d[2] = w[2]; d[3] = w[3];
   }
@@ -163,7 +167,8 @@ __global__ __launch_bounds__(256) void rearrange_kv_kernel(Geo g, OrderJob job, 
   for (int r = 0; r < (K ? 4 : 0); ++r) {
     const int oc = tid + 256 * r;
     const int lane = oc & 63, s = (oc >> 6) & 3, kt16 = oc >> 8;
-    kp[tile * 1024 + oc] = *(const u32x4*)(kt + (size_t)(16 * kt16 + (lane & 15)) * lk.st + 32 * s + 8 * (lane >> 4));
+    const int row = 16 * kt16 + (lane & 15);
+    kp[tile * 1024 + oc] = *(const u32x4*)(kt + (size_t)(ODD ? min(row, part.y - 1) : row) * lk.st + 32 * s + 8 * (lane >> 4));
   }
   if constexpr (!V) return;
   __syncthreads();
@@ -284,7 +289,9 @@ __device__ __forceinline__ int next_in_queue(const RowFilter& flt, int n_kvh, in
 // registers (bf16 304, int8 268, FP8 270) against 393 - 449, where two waves would need 256 or less.  So a row gains because
 // its work is on two SIMDs, not because one wave covers the other's latency.  A query's arithmetic is the same in both, bit
 // for bit.
-template <int WAVES, bool BK32, bool QK8, bool PV8 = false, int NT = 2>
+// ODD: sequences of any length (Geo::tokens_of; dense bf16).  The rows behind a sequence's last token repeat its last query
+// and are not stored; the keys there come after every query.
+template <int WAVES, bool BK32, bool QK8, bool PV8 = false, int NT = 2, bool ODD = false>
 __global__ __launch_bounds__(WAVES * (2 / NT) * 64) void attn_rows_kernel(Geo g, const uint16_t* __restrict__ q,
                                                                const bf16x8* __restrict__ kp,
                                                                const bf16x8* __restrict__ vp, Qk8 q8o,
@@ -296,6 +303,7 @@ __global__ __launch_bounds__(WAVES * (2 / NT) * 64) void attn_rows_kernel(Geo g,
                                                                RowFilter flt, f32x4* __restrict__ st_o,
                                                                float* __restrict__ st_ml) {
   static_assert(NT == 2 || WAVES == 1, "the two halves of a row share a workgroup of their own");
+  static_assert(!ODD || (!BK32 && !QK8), "sequences of any length: dense, bf16");
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave_id = __builtin_amdgcn_readfirstlane(tid >> 6);      // (wave-uniform by construction: the unit and its addresses are scalars)
   const int wave = NT == 1 ? 0 : wave_id;
@@ -333,6 +341,7 @@ __global__ __launch_bounds__(WAVES * (2 / NT) * 64) void attn_rows_kernel(Geo g,
 
   // ---- this wave's list of kept blocks: the set bits of its mask row, below the diagonal ----
   const uint64_t* mrow = mask ? mask + ((size_t)u.qh * g.n_qb + u.i) * g.words : nullptr;
+  const int2 part = ODD ? g.tokens_of[u.i] : make_int2(u.i * 64, 64);      // first token of the row block, and how many
   const SeqPos sp = seq_pos(g, u.i);                // (variable-length batches: block indices inside the row's sequence)
   const int il = sp.il;
   const int j_last = BK32 ? 2 * il + 1 : il;        // last causally visible mask bit of the row
@@ -378,7 +387,8 @@ __global__ __launch_bounds__(WAVES * (2 / NT) * 64) void attn_rows_kernel(Geo g,
 #pragma unroll
         for (int s = 0; s < 2; ++s) qf8[qt][s] = *(const i32x4*)(row + 64 * s);
       } else {
-        const uint16_t* row = q + row_off(g.sq, u.qh, u.i * 64 + q0 + 16 * qt + n16) + 8 * g16;
+        const int r = q0 + 16 * qt + n16;
+        const uint16_t* row = q + row_off(g.sq, u.qh, part.x + (ODD ? min(r, part.y - 1) : r)) + 8 * g16;
 #pragma unroll
         for (int s = 0; s < 4; ++s) qf[qt][s] = *(const bf16x8*)(row + 32 * s);
       }
@@ -825,6 +835,42 @@ __global__ __launch_bounds__(WAVES * (2 / NT) * 64) void attn_rows_kernel(Geo g,
     due = 0;
   };
 
+  // (ODD) The product O += V P of a half-tile of the diagonal block whose V holds an infinity or a NaN: zero times these is NaN,
+  // so it is taken key by key for the queries that see the key; V is zero afterwards.  koff as in hide.
+  auto key_by_key = [&](int y, int koff) __attribute__((always_inline)) {
+    uint32_t odd = 0;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t x = __builtin_bit_cast(u32x4, vf[y][dt])[w];
+        odd |= (((x & 0x7F800000u) + 0x00800000u) | ((x << 16 & 0x7F800000u) + 0x00800000u)) & 0x80000000u;
+      }
+    if (__builtin_expect_with_probability(__builtin_amdgcn_ballot_w64(odd != 0) != 0, 0, 0.999)) {
+#pragma clang loop unroll(disable)
+      for (int key = 0; key < 32; ++key) {
+        const int at = (key >> 2 & 3) == g16 ? 4 * (key >> 4) + (key & 3) : -1;      // (layout of V': see rearrange_kv_kernel)
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+          bf16x8 one;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) one[e] = e == at ? vf[y][dt][e] : (__bf16)0.0f;
+#pragma unroll
+          for (int qt = 0; qt < NQ; ++qt) {
+            const f32x4 t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, P[y][qt], f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (koff + key <= q0 + 16 * qt + n16) o16[dt][qt][r] += t[r];
+          }
+        }
+      }
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vf[y][dt][e] = (__bf16)0.0f;
+    }
+  };
+
   struct Pair { int a, b; float ka, kb; };      // half-tiles of the two slots; QK8: the K scales of their blocks
   // One phase.  x: slot whose probabilities are made; y = 1 - x: slot of the two products and of the loads.  more: the scores
   // made here are complete (no key of theirs is to be hidden), so that their maximum counts.
@@ -937,9 +983,11 @@ __global__ __launch_bounds__(WAVES * (2 / NT) * 64) void attn_rows_kernel(Geo g,
       look_at(0, factor(c0.ka));
     }
     phase(slot0, c0.ka, c0.b, c0.b, c0.kb, false);
+    if constexpr (ODD) key_by_key(0, (c0.a - 2 * il) * 32);
     hide(1, (c0.b - 2 * il) * 32);
     look_at(1, factor(c0.kb));
     phase(slot1, c0.kb, c0.b, c0.b, c0.ka, false);
+    if constexpr (ODD) key_by_key(1, (c0.b - 2 * il) * 32);
 #pragma unroll
     for (int n = 0; n < kPv; ++n) pv_mfma(1, n);
 #pragma unroll
@@ -994,7 +1042,8 @@ __global__ __launch_bounds__(WAVES * (2 / NT) * 64) void attn_rows_kernel(Geo g,
     }
   };
   auto put_lse = [&](int r, float m, float l_tot) __attribute__((always_inline)) {
-    const size_t row = (size_t)u.qh * g.seq + u.i * 64 + q0 + r;
+    if (ODD && q0 + r >= part.y) return;
+    const size_t row = (size_t)u.qh * (ODD ? g.tokens : g.seq) + part.x + q0 + r;
     // (PV8: the sum is that of 448 p)
     // (the FMA is spelled out so that every instance of the kernel rounds alike)
     float v = l_tot > 0.0f ? __builtin_fmaf(m, 0.6931471805599453f, __logf(PV8 ? l_tot * (1.0f / 448.0f) : l_tot)) : -INFINITY;
@@ -1039,11 +1088,11 @@ __global__ __launch_bounds__(WAVES * (2 / NT) * 64) void attn_rows_kernel(Geo g,
   if (!o32) {
     // (each wave reads back only its own tile: no barrier, LDS operations of a wave complete in order)
     wave_exchange();
-    uint16_t* const out = o + row_off(g.so, u.qh, u.i * 64 + q0);
+    uint16_t* const out = o + row_off(g.so, u.qh, part.x + q0);
 #pragma unroll
     for (int it = 0; it < 8 * NT; ++it) {
       const int r = 4 * it + (lane >> 4), ch = 8 * (lane & 15);
-      *(u32x4*)(out + (size_t)r * g.so.st + ch) = *(const u32x4*)(tile + r * kRowPad + ch);
+      if (!ODD || q0 + r < part.y) *(u32x4*)(out + (size_t)r * g.so.st + ch) = *(const u32x4*)(tile + r * kRowPad + ch);
     }
   }
 }
@@ -1455,9 +1504,161 @@ int launch_attn_rows(const sale_params_t* p, const void* q, const void* k, const
              : launch_dense_rows<false, false>(g, qq, kpp, vpp, q8o, order, (uint16_t*)o, o32, lse, halves, st);
 }
 
+// ---- prompts of any length ----------------------------------------------------------------------------------
+// The kernels above work on 64-row blocks of ONE sequence.  Here the blocks of all sequences, each of whose last one may be
+// partly filled, follow each other; a table says which tokens a block holds.  K' and V' are made for whole blocks (V' zero
+// behind the last token), so the sweep itself is that of the dense kernel, instruction for instruction; only Q, O and lse
+// are addressed by token, and what is not finite in V is kept from queries before its key (key_by_key).
+namespace {
+
+constexpr int kTokenChunk = 255;
+struct TokenChunk {
+  int n;
+  int block[kTokenChunk + 1];      // first block of every sequence of the chunk, and the end of the last
+  int token[kTokenChunk + 1];      // first token, likewise
+};
+
+__global__ __launch_bounds__(256) void token_table_kernel(TokenChunk c, int32_t* __restrict__ seq_start, int2* __restrict__ tokens_of) {
+  const int b = c.block[0] + blockIdx.x * 256 + threadIdx.x;
+  if (b >= c.block[c.n]) return;
+  int lo = 0, hi = c.n;      // the last sequence that starts at block b or before: the one that has it
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (c.block[mid] <= b) lo = mid; else hi = mid;
+  }
+  const int t = c.token[lo] + 64 * (b - c.block[lo]);
+  seq_start[b] = c.block[lo];
+  tokens_of[b] = make_int2(t, min(64, c.token[lo + 1] - t));
+}
+
+struct PromptShape {
+  long long blocks;         // 64-row blocks of one head
+  int longest;              // of the longest sequence
+  long even_rows;           // as in BatchShape, all heads
+  bool long_rows_wait;
+};
+// f(first token, end) for every sequence, last one first
+template <class F>
+void for_sequences_from_last(const sale_params_t* p, F f) {
+  if (p->n_seqs <= 0) { f(0, p->seq_len); return; }
+  for (int s = p->n_seqs - 1; s >= 0; --s) f(p->cu_seqlens[s], p->cu_seqlens[s + 1]);
+}
+PromptShape prompt_shape(const sale_params_t* p) {
+  PromptShape s = {0, 0, 0, false};
+  auto blocks_of = [](int a, int z) { return (z - a + kBlockQ - 1) / kBlockQ; };
+  long long work = 0;
+  for_sequences_from_last(p, [&](int a, int z) {
+    const int n = blocks_of(a, z);
+    s.blocks += n;
+    s.longest = n > s.longest ? n : s.longest;
+    work += (long long)n * (n + 1);
+  });
+  const long long heads = (long long)p->batch * p->n_q_heads;
+  s.even_rows = (long)(heads * work / (s.longest + 1));
+  long long after = 0;
+  if (p->n_seqs > 0)
+    for_sequences_from_last(p, [&](int a, int z) {
+      const int n = blocks_of(a, z);
+      if (4LL * n >= 3LL * s.longest) s.long_rows_wait = heads * after >= 512;
+      after += n;
+    });
+  return s;
+}
+
+struct PromptWs {
+  u32x4 *kp, *vp;
+  int2* tokens_of;
+  int32_t *seq_start, *order;
+  size_t bytes;
+};
+PromptWs carve_prompt_ws(const sale_params_t* p, const PromptShape& s, void* base) {
+  PromptWs w = {};
+  size_t off = 0;
+  auto take = [&](size_t bytes) { uint8_t* ptr = (uint8_t*)base + off; off += (bytes + 63) & ~(size_t)63; return ptr; };
+  const size_t copy = (size_t)p->batch * p->n_kv_heads * (size_t)s.blocks * 64 * kHeadDim * sizeof(uint16_t);
+  w.kp = (u32x4*)take(copy);
+  w.vp = (u32x4*)take(copy);
+  w.tokens_of = (int2*)take((size_t)s.blocks * sizeof(int2));
+  w.seq_start = (int32_t*)take((size_t)s.blocks * sizeof(int32_t));
+  w.order = (int32_t*)take((size_t)p->batch * p->n_q_heads * (size_t)s.blocks * sizeof(int32_t));
+  w.bytes = off;
+  return w;
+}
+
+int validate_prompt(const sale_params_t* p) {
+  const int rc = validate_tokens(p);
+  if (rc != SALE_OK) return rc;
+  const PromptShape s = prompt_shape(p);
+  if (s.longest > kMaxSeqLen / kBlockQ) return SALE_ERR_UNSUPPORTED;
+  if (s.blocks * p->batch * p->n_q_heads > 0x3FFFFFFFLL || s.blocks > 0x1FFFFFFLL) return SALE_ERR_UNSUPPORTED;      // (32-bit indices)
+  return SALE_OK;
+}
+
+}  // namespace
+
+size_t prompt_workspace_bytes(const sale_params_t* p) {
+  return validate_prompt(p) == SALE_OK ? carve_prompt_ws(p, prompt_shape(p), nullptr).bytes : 0;
+}
+
 }  // namespace sale
 
 using namespace sale;
+
+extern "C" int sale_prompt_attn(const sale_params_t* p, const void* q, const void* k, const void* v, void* o, float* lse,
+                                void* ws, size_t ws_bytes, void* stream) {
+  if (!p || !q || !k || !v || !o) return SALE_ERR_NULL_ARG;
+  int rc = validate_prompt(p);
+  if (rc != SALE_OK) return rc;
+  if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)o) & 15) return SALE_ERR_BAD_SHAPE;
+  const PromptShape shape = prompt_shape(p);
+  const PromptWs w = carve_prompt_ws(p, shape, ws);
+  if (!ws || ws_bytes < w.bytes || ((uintptr_t)ws & 15)) return SALE_ERR_WORKSPACE;
+  const hipStream_t st = (hipStream_t)stream;
+  sale_params_t blocks = *p;      // (the caller's block sizes are not read)
+  blocks.block_q = kBlockQ;
+  blocks.block_k = kBlockK;
+  Geo g = make_geo(&blocks);
+  g.n_qb = g.n_kb = (int)shape.blocks;
+  g.seq = g.n_qb * kBlockQ;
+  g.words = (shape.longest + 63) / 64;
+  g.seq_start = w.seq_start;
+  g.tokens_of = w.tokens_of;
+  const int n_seqs = p->n_seqs > 0 ? p->n_seqs : 1;
+  const int whole[2] = {0, p->seq_len};
+  const int32_t* offsets = p->n_seqs > 0 ? p->cu_seqlens : whole;
+  int block = 0;
+  for (int s0 = 0; s0 < n_seqs; s0 += kTokenChunk) {
+    TokenChunk c;
+    c.n = min(kTokenChunk, n_seqs - s0);
+    const int first = block;
+    for (int e = 0; e <= c.n; ++e) {
+      if (e > 0) block += (offsets[s0 + e] - offsets[s0 + e - 1] + kBlockQ - 1) / kBlockQ;
+      c.block[e] = block;
+      c.token[e] = offsets[s0 + e];
+    }
+    if (block == first) continue;      // (sequences of no tokens)
+    token_table_kernel<<<dim3((unsigned)((block - first + 255) / 256)), dim3(256), 0, st>>>(c, w.seq_start, w.tokens_of);
+    if (hipGetLastError() != hipSuccess) return SALE_ERR_HIP;
+  }
+  const long n_units = (long)g.n_qh * g.n_qb;
+  bool halves = two_waves_per_row({n_units, shape.even_rows, shape.longest, g.n_kvh, g.group, true, false, false, false, p->n_seqs > 0});
+  const bool sort = halves && shape.long_rows_wait;
+  const OrderJob job = {sort ? g.n_kvh : 0, nullptr, nullptr, w.order};
+  rearrange_kv_kernel<true, true, true><<<dim3((unsigned)(job.heads + g.n_kvh * g.n_qb)), dim3(256), 0, st>>>(
+      g, job, NoPass8{}, (const uint16_t*)k, (const uint16_t*)v, w.kp, w.vp, nullptr);
+  if (hipGetLastError() != hipSuccess) return SALE_ERR_HIP;
+  const int units = g.n_qb * g.group;
+  const Qk8 none = {nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
+  const RowFilter all = {nullptr, -1, 0, -1, 0, 0};
+#define SALE_PROMPT_ARGS g, (const uint16_t*)q, (const bf16x8*)w.kp, (const bf16x8*)w.vp, none, nullptr, sort ? w.order : nullptr, nullptr, \
+                         (uint16_t*)o, nullptr, lse, all, nullptr, nullptr
+  if (halves)
+    attn_rows_kernel<1, false, false, false, 1, true><<<dim3((unsigned)(units * g.n_kvh)), dim3(128), 0, st>>>(SALE_PROMPT_ARGS);
+  else
+    attn_rows_kernel<4, false, false, false, 2, true><<<dim3((unsigned)(((units + 3) / 4) * g.n_kvh)), dim3(256), 0, st>>>(SALE_PROMPT_ARGS);
+#undef SALE_PROMPT_ARGS
+  return hipGetLastError() == hipSuccess ? SALE_OK : SALE_ERR_HIP;
+}
 
 extern "C" int sale_sparse_attn(const sale_params_t* p, const void* q, const void* k, const void* v,
                                 const uint64_t* block_mask, const int32_t* row_counts, void* o, float* lse, void* ws,

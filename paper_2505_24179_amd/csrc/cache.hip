@@ -1,0 +1,252 @@
+// Pages of a cache: writing new tokens into them, and copying them.  Both only move bytes (8-bit pages: and round them), so
+// what bounds them is HBM, or latency where a call is a few megabytes or less.
+#include <stdlib.h>
+
+#include "cache.h"
+
+namespace sale {
+
+int validate_cache(const sale_params_t* p, const sale_cache_t* c, bool tables) {
+  if (!c->k || !c->v) return SALE_ERR_NULL_ARG;
+  if (c->dtype != SALE_PAGE_BF16 && c->dtype != SALE_PAGE_FP8) return SALE_ERR_UNSUPPORTED;
+  if (c->n_pages <= 0 || c->page_tokens <= 0) return SALE_ERR_BAD_SHAPE;
+  if (c->page_tokens < 16 || c->page_tokens > 256 || (c->page_tokens & (c->page_tokens - 1))) return SALE_ERR_UNSUPPORTED;
+  if (((uintptr_t)c->k | (uintptr_t)c->v) & 15) return SALE_ERR_BAD_SHAPE;
+  const int unit = c->dtype == SALE_PAGE_FP8 ? 16 : 8;      // elements of 16 bytes
+  const int64_t* triples[2] = {c->k_stride, c->v_stride};
+  for (const int64_t* st : triples) {
+    if (st[0] == 0 && st[1] == 0 && st[2] == 0) continue;
+    for (int e = 0; e < 3; ++e)
+      if (st[e] < 0 || st[e] % unit) return SALE_ERR_BAD_SHAPE;
+    if (st[2] < kHeadDim || st[2] > (1 << 24)) return SALE_ERR_BAD_SHAPE;
+    if ((p->n_kv_heads > 1 && st[1] == 0) || (c->n_pages > 1 && st[0] == 0)) return SALE_ERR_BAD_SHAPE;
+  }
+  if (c->dtype == SALE_PAGE_FP8 && tables && (!c->k_scale || !c->v_scale)) return SALE_ERR_NULL_ARG;
+  if (!tables) return SALE_OK;
+  if (!c->table || !c->lens) return SALE_ERR_NULL_ARG;
+  if (c->table_width <= 0) return SALE_ERR_BAD_SHAPE;
+  if ((long long)c->table_width * c->page_tokens > 0x3FFFFFFF) return SALE_ERR_UNSUPPORTED;      // positions are 32-bit
+  return SALE_OK;
+}
+
+CacheView cache_view(const sale_params_t* p, const sale_cache_t* c) {
+  const long long size = c->dtype == SALE_PAGE_FP8 ? 1 : 2;
+  auto side = [&](void* base, const int64_t* st) -> PageSide {
+    if (st[0] == 0 && st[1] == 0 && st[2] == 0) {
+      const long long token = kHeadDim * size, head = token * c->page_tokens;
+      return {(uint8_t*)base, head * p->n_kv_heads, head, token};
+    }
+    return {(uint8_t*)base, st[0] * size, st[1] * size, st[2] * size};
+  };
+  return {side(c->k, c->k_stride), side(c->v, c->v_stride), c->k_scale, c->v_scale, c->table, c->lens, c->n_pages,
+          __builtin_ctz((unsigned)c->page_tokens), c->table_width};
+}
+
+namespace {
+
+// ---- append ------------------------------------------------------------------------------------------------
+// A workgroup takes up to `tile` tokens of one sequence, all KV heads, K and V: 16 bytes (8 channels) of the new token per
+// thread and turn, so that a row of 256 bytes is 16 neighbouring threads'.  Where the tokens of a sequence lie among the
+// packed ones travels with the launch, up to kAppendChunk sequences at a time.
+constexpr int kAppendChunk = 255;
+struct AppendJob {
+  CacheView c;
+  const uint8_t *k, *v;
+  Strided sk, sv;
+  int n_kvh, tile, heads_first;      // heads_first: neighbouring rows are those of neighbouring heads
+  int each, tiles_each;              // > 0: every sequence has that many new tokens, and workgroups; otherwise by `at`
+  int first_seq, n;
+  int token[kAppendChunk + 1], at[kAppendChunk + 1];      // first token and first workgroup of a sequence
+};
+
+// e4m3 of two values: nearest, ties to even; at most 448 in size; NaN stays.
+__device__ __forceinline__ float limit448(float x) { return x != x ? x : fminf(fmaxf(x, -448.0f), 448.0f); }
+__device__ __forceinline__ u32x2 to_fp8(u32x4 w, float scale) {
+  u32x2 out;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    int r = 0;
+    float x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t word = w[2 * h + (e >> 1)];
+      x[e] = limit448(__builtin_bit_cast(float, e & 1 ? word & 0xFFFF0000u : word << 16) / scale);
+    }
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], r, false);
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], r, true);
+    out[h] = (uint32_t)r;
+  }
+  return out;
+}
+
+template <bool FP8>
+__global__ __launch_bounds__(256) void append_kernel(AppendJob a) {
+  int s, t0, n_new, first;      // sequence, first token of the tile in it, its new tokens, its first packed token
+  if (a.each > 0) {
+    s = blockIdx.x / a.tiles_each;
+    t0 = (int)(blockIdx.x - s * a.tiles_each) * a.tile;
+    n_new = a.each;
+    first = 0;      // (of batch entry s)
+  } else {
+    int lo = 0, hi = a.n;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (a.at[mid] <= (int)blockIdx.x) lo = mid; else hi = mid;
+    }
+    s = a.first_seq + lo;
+    t0 = ((int)blockIdx.x - a.at[lo]) * a.tile;
+    first = a.token[lo];
+    n_new = a.token[lo + 1] - first;
+  }
+  const int count = min(a.tile, n_new - t0), rows = count * a.n_kvh;
+  const int start = max(a.c.lens[s], 0) - n_new;      // position of the sequence's first new token
+  const int32_t* table = a.c.table + (size_t)s * a.c.width;
+  const int batch = a.each > 0 ? s : 0;
+  for (int id = threadIdx.x; id < 2 * rows * 16; id += 256) {
+    const bool is_v = id >= rows * 16;
+    const int row = (is_v ? id - rows * 16 : id) >> 4, chunk = id & 15;
+    const int h = a.heads_first ? row % a.n_kvh : row / count, i = a.heads_first ? row / a.n_kvh : row % count;
+    const int pos = start + t0 + i;
+    if (pos < 0 || pos >> a.c.page_shift >= a.c.width) continue;
+    const int page = table[pos >> a.c.page_shift], slot = pos & ((1 << a.c.page_shift) - 1);
+    if ((unsigned)page >= (unsigned)a.c.n_pages) continue;
+    const Strided& ss = is_v ? a.sv : a.sk;
+    const size_t from = 2 * ((size_t)batch * ss.sb + (size_t)h * ss.sh + (size_t)(first + t0 + i) * ss.st) + 16 * chunk;
+    const u32x4 w = *(const u32x4*)((is_v ? a.v : a.k) + from);
+    const PageSide& side = is_v ? a.c.v : a.c.k;
+    uint8_t* to = side.base + (long long)page * side.page + (long long)h * side.head + (long long)slot * side.token;
+    if constexpr (FP8) *(u32x2*)(to + 8 * chunk) = to_fp8(w, (is_v ? a.c.v_scale : a.c.k_scale)[h]);
+    else *(u32x4*)(to + 16 * chunk) = w;
+  }
+}
+
+// ---- copy --------------------------------------------------------------------------------------------------
+// Pairs of pages travel with the launch, kCopyChunk at a time.  A workgroup copies 16 KB of K or of V, 4 loads of 16 bytes
+// per thread in flight.
+constexpr int kCopyChunk = 448;
+constexpr int kCopyBytes = 16384;
+struct CopyJob {
+  PageSide k, v;
+  int parts;              // workgroups per page and side
+  int row_shift;          // log2 of the 16-byte pieces of a token's row
+  int page_shift, n_kvh;
+  int heads_first;
+  int src[kCopyChunk], dst[kCopyChunk];
+};
+
+__global__ __launch_bounds__(256) void copy_kernel(CopyJob a) {
+  const int pair = blockIdx.x / (2 * a.parts), part = blockIdx.x % (2 * a.parts);
+  const PageSide& side = part < a.parts ? a.k : a.v;
+  const uint8_t* from = side.base + (long long)a.src[pair] * side.page;
+  uint8_t* to = side.base + (long long)a.dst[pair] * side.page;
+  const int pieces = a.n_kvh << (a.page_shift + a.row_shift), tokens = 1 << a.page_shift;
+  const int first = (part < a.parts ? part : part - a.parts) * (kCopyBytes / 16) + (int)threadIdx.x;
+  u32x4 w[4];
+  long long at[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int piece = first + 256 * r, row = piece >> a.row_shift;
+    const int h = a.heads_first ? row % a.n_kvh : row >> a.page_shift, slot = a.heads_first ? row / a.n_kvh : row & (tokens - 1);
+    at[r] = (long long)h * side.head + (long long)slot * side.token + 16 * (piece & ((1 << a.row_shift) - 1));
+    if (piece < pieces) w[r] = *(const u32x4*)(from + at[r]);
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (first + 256 * r < pieces) *(u32x4*)(to + at[r]) = w[r];
+}
+
+// All pages in range, the destinations different and none a source.  (One bit per page in each of two sets; < 0: SALE_ERR_*)
+int check_pairs(const int32_t* src, const int32_t* dst, int n, int n_pages) {
+  const size_t words = ((size_t)n_pages + 63) / 64;
+  uint64_t* const sets = (uint64_t*)calloc(2 * words, sizeof(uint64_t));
+  if (!sets) return SALE_ERR_HIP;
+  uint64_t *const is_src = sets, *const is_dst = sets + words;
+  int rc = SALE_OK;
+  for (int i = 0; i < n && rc == SALE_OK; ++i) {
+    if (src[i] < 0 || src[i] >= n_pages || dst[i] < 0 || dst[i] >= n_pages) { rc = SALE_ERR_BAD_SHAPE; break; }
+    const uint64_t bit = 1ull << (dst[i] & 63);
+    if (is_dst[dst[i] >> 6] & bit) rc = SALE_ERR_BAD_SHAPE;
+    is_dst[dst[i] >> 6] |= bit;
+    is_src[src[i] >> 6] |= 1ull << (src[i] & 63);
+  }
+  for (size_t w = 0; w < words && rc == SALE_OK; ++w)
+    if (is_src[w] & is_dst[w]) rc = SALE_ERR_BAD_SHAPE;
+  free(sets);
+  return rc;
+}
+
+}  // namespace
+}  // namespace sale
+
+using namespace sale;
+
+extern "C" int sale_cache_append(const sale_params_t* p, const sale_cache_t* cache, const void* k, const void* v, void* stream) {
+  if (!p || !cache || !k || !v) return SALE_ERR_NULL_ARG;
+  int rc = validate_tokens(p);
+  if (rc == SALE_OK) rc = validate_cache(p, cache, true);
+  if (rc != SALE_OK) return rc;
+  if (((uintptr_t)k | (uintptr_t)v) & 15) return SALE_ERR_BAD_SHAPE;
+  AppendJob a;
+  a.c = cache_view(p, cache);
+  a.k = (const uint8_t*)k;
+  a.v = (const uint8_t*)v;
+  a.sk = layout_of(p->k_stride, p->n_kv_heads, p->seq_len);
+  a.sv = layout_of(p->v_stride, p->n_kv_heads, p->seq_len);
+  a.n_kvh = p->n_kv_heads;
+  a.heads_first = a.sk.sh < a.sk.st ? 1 : 0;
+  a.tile = 64 / p->n_kv_heads < 1 ? 1 : 64 / p->n_kv_heads;      // 8 turns of a workgroup
+  const hipStream_t st = (hipStream_t)stream;
+  auto launch = [&](long long workgroups) -> int {
+    if (workgroups > 0x7FFFFFFF) return SALE_ERR_UNSUPPORTED;
+    if (cache->dtype == SALE_PAGE_FP8) append_kernel<true><<<dim3((unsigned)workgroups), dim3(256), 0, st>>>(a);
+    else append_kernel<false><<<dim3((unsigned)workgroups), dim3(256), 0, st>>>(a);
+    return hipGetLastError() == hipSuccess ? SALE_OK : SALE_ERR_HIP;
+  };
+  a.each = a.tiles_each = 0;
+  if (p->n_seqs == 0) {
+    a.each = p->seq_len;
+    a.tiles_each = (p->seq_len - 1) / a.tile + 1;
+    return launch((long long)a.tiles_each * p->batch);
+  }
+  for (int s0 = 0; s0 < p->n_seqs; s0 += kAppendChunk) {
+    a.first_seq = s0;
+    a.n = min(kAppendChunk, p->n_seqs - s0);
+    int at = 0;
+    for (int e = 0; e <= a.n; ++e) {
+      a.token[e] = p->cu_seqlens[s0 + e];
+      if (e > 0) at += (a.token[e] - a.token[e - 1] + a.tile - 1) / a.tile;
+      a.at[e] = at;
+    }
+    if (at > 0 && (rc = launch(at)) != SALE_OK) return rc;
+  }
+  return SALE_OK;
+}
+
+extern "C" int sale_cache_copy(const sale_params_t* p, const sale_cache_t* cache, const int32_t* src, const int32_t* dst,
+                               int32_t n, void* stream) {
+  if (!p || !cache || (n > 0 && (!src || !dst))) return SALE_ERR_NULL_ARG;
+  if (p->n_kv_heads <= 0 || n < 0) return SALE_ERR_BAD_SHAPE;
+  if (p->head_dim != kHeadDim) return SALE_ERR_UNSUPPORTED;
+  int rc = validate_cache(p, cache, false);
+  if (rc == SALE_OK) rc = check_pairs(src, dst, n, cache->n_pages);
+  if (rc != SALE_OK) return rc;
+  const CacheView c = cache_view(p, cache);
+  CopyJob a;
+  a.k = c.k;
+  a.v = c.v;
+  a.row_shift = cache->dtype == SALE_PAGE_FP8 ? 3 : 4;
+  a.page_shift = c.page_shift;
+  a.n_kvh = p->n_kv_heads;
+  a.heads_first = c.k.head < c.k.token ? 1 : 0;
+  const long long page_bytes = (long long)p->n_kv_heads * cache->page_tokens << (a.row_shift + 4);
+  if (page_bytes > (1LL << 30)) return SALE_ERR_UNSUPPORTED;      // (pieces of a launch are counted in 32 bits)
+  a.parts = (int)((page_bytes + kCopyBytes - 1) / kCopyBytes);
+  const int chunk = (int)min((long long)kCopyChunk, max(1LL, 0x7FFFFFFFLL / (2LL * a.parts)));
+  for (int i0 = 0; i0 < n; i0 += chunk) {
+    const int m = min(chunk, n - i0);
+    for (int i = 0; i < m; ++i) { a.src[i] = src[i0 + i]; a.dst[i] = dst[i0 + i]; }
+    copy_kernel<<<dim3((unsigned)(m * 2 * a.parts)), dim3(256), 0, (hipStream_t)stream>>>(a);
+    if (hipGetLastError() != hipSuccess) return SALE_ERR_HIP;
+  }
+  return SALE_OK;
+}

@@ -68,6 +68,11 @@ struct Geo {
   // nullptr when every (batch, head) is one sequence.  n_qb, n_kb, seq then count the packed total and
   // `words` the mask words of the longest sequence.
   const int32_t* seq_start;
+  // Sequences of any length (prompt_attn): [n_qb] first token and number of tokens of every block (a sequence's last one may
+  // hold fewer than 64), and the tokens of a head.  The blocks of all sequences then follow each other, n_qb, n_kb and seq
+  // count whole blocks, and seq_start is always there.  nullptr: block i holds tokens 64 i .. 64 i + 63.
+  const int2* tokens_of;
+  int tokens;
 };
 
 // Query block i of the packed token axis -> (its index inside its sequence, first key block of that sequence).
@@ -190,6 +195,9 @@ __device__ __forceinline__ Unit unit_of(const Geo& g, int block, int wave) {
 // and at most 4096 key blocks (everything else).
 enum GeomClass { kGeomQuantize, kGeomPath };
 int validate_common(const sale_params_t* p, GeomClass cls);
+int validate_tokens(const sale_params_t* p);      // the serving calls: any length, no blocks, no flags
+Strided layout_of(const int64_t* stride, int heads, int seq_len);      // all-zero strides: contiguous
+size_t prompt_workspace_bytes(const sale_params_t* p);      // 0 if the parameters are invalid
 // attention launcher shared by the attention entry points and the calibration (attention.hip)
 int launch_attn_rows(const sale_params_t* p, const void* q, const void* k, const void* v, const uint64_t* mask,
                      const int32_t* row_counts, void* o, float* o32, float* lse, void* ws, size_t ws_bytes, hipStream_t st);

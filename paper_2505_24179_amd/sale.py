@@ -33,6 +33,7 @@ WS_CALIBRATE = 4
 WS_INT8_OPERANDS = 5
 WS_FP8_OPERANDS = 6
 WS_SPARSE_ATTN_MIN = 7
+WS_PROMPT_ATTN = 8
 PARKED_ROW_BYTES = 33792      # one parking slot of sparse_attn's workspace (see include/sale.h)
 
 
@@ -116,8 +117,84 @@ class Params:
         return (longest // self.block_k + 63) // 64
 
 
+class _Cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + \
+        [(n, ctypes.c_int64 * 3) for n in ("k_stride", "v_stride")] + \
+        [(n, ctypes.c_int32) for n in ("n_pages", "page_tokens", "dtype", "table_width")] + \
+        [(n, ctypes.c_void_p) for n in ("table", "lens")]
+
+
+PAGE_BF16 = 0
+PAGE_FP8 = 1
+
+
+@dataclass(frozen=True, eq=False)
+class Cache:
+    """Keys and values of many sequences in pages (see include/sale.h): tensors that the program owns and fills as it likes.
+
+    k, v             [pages, KV heads, tokens of a page, head_dim], torch.bfloat16 or torch.float8_e4m3fn, of any strides whose
+                     last dimension is contiguous
+    table            int32 [sequences, width]: the pages of each sequence in order, -1 (or anything that is no page) where
+                     there is none
+    lens             int32 [sequences]: tokens that each sequence holds
+    k_scale, v_scale fp32 [KV heads], 8-bit pages only: a key is value * k_scale
+
+    Forking a sequence is copying its row of `table` and `lens` and, if its last page is partly filled, that page
+    (`cache_copy`) to a fresh one; freeing is handing its pages to others; compacting is `cache_copy` and new numbers in `table`."""
+    k: torch.Tensor
+    v: torch.Tensor
+    table: torch.Tensor
+    lens: torch.Tensor
+    k_scale: torch.Tensor = None
+    v_scale: torch.Tensor = None
+
+    def __post_init__(self):
+        for name, t in (("k", self.k), ("v", self.v)):
+            if not t.is_cuda:
+                raise ValueError(f"{name}: expected a device tensor, got {t.device}")
+            if t.dtype not in (torch.bfloat16, torch.float8_e4m3fn) or t.dtype != self.k.dtype:
+                raise ValueError(f"{name}: expected pages of torch.bfloat16 or torch.float8_e4m3fn, K and V alike, got {t.dtype}")
+            if t.dim() != 4 or t.shape != self.k.shape or t.numel() == 0:
+                raise ValueError(f"{name}: expected [pages, KV heads, tokens, head_dim], K and V alike, got {tuple(t.shape)}")
+            if t.stride(3) != 1:
+                raise ValueError(f"{name}: the last dimension has to be contiguous, got strides {t.stride()}")
+        if self.table.dim() != 2:
+            raise ValueError(f"table: expected [sequences, pages], got {tuple(self.table.shape)}")
+        _expect("table", self.table, torch.int32, self.table.numel())
+        _expect("lens", self.lens, torch.int32, self.table.shape[0])
+        if self.k.dtype == torch.float8_e4m3fn:
+            _expect("k_scale", self.k_scale, torch.float32, self.k.shape[1])
+            _expect("v_scale", self.v_scale, torch.float32, self.k.shape[1])
+        for name in ("v", "table", "lens", "k_scale", "v_scale"):
+            t = getattr(self, name)
+            if t is not None and t.device != self.k.device:
+                raise ValueError(f"{name}: on {t.device}, the pages of K on {self.k.device}")
+
+    @cached_property
+    def _struct(self):
+        c = _Cache(n_pages=self.k.shape[0], page_tokens=self.k.shape[2], table_width=self.table.shape[1],
+                   dtype=PAGE_FP8 if self.k.dtype == torch.float8_e4m3fn else PAGE_BF16)
+        for name, t in (("k_stride", self.k), ("v_stride", self.v)):
+            if not t.is_contiguous():
+                getattr(c, name)[:] = t.stride()[:3]
+        return c
+
+    def _arg(self, p: "Params", sequences=None):
+        """The C struct, as an argument of a call with parameters p (over so many sequences)."""
+        shape = self.k.shape
+        if shape[1] != p.n_kv_heads or shape[3] != p.head_dim:
+            raise ValueError(f"cache: pages of {shape[1]} KV heads x {shape[3]} channels, the call has {p.n_kv_heads} x {p.head_dim}")
+        if sequences is not None and self.table.shape[0] != sequences:
+            raise ValueError(f"cache: a table of {self.table.shape[0]} sequences, the call has {sequences}")
+        c = self._struct
+        c.k, c.v, c.table, c.lens = self.k.data_ptr(), self.v.data_ptr(), self.table.data_ptr(), self.lens.data_ptr()
+        if c.dtype == PAGE_FP8:
+            c.k_scale, c.v_scale = self.k_scale.data_ptr(), self.v_scale.data_ptr()
+        return ctypes.byref(c)
+
+
 _vp, _sz, _i32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32
-_pp = ctypes.POINTER(_Params)
+_pp, _pc = ctypes.POINTER(_Params), ctypes.POINTER(_Cache)
 _SIGS = {
     "sale_workspace_bytes": (_sz, [_pp, ctypes.c_int]),
     "sale_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -131,6 +208,11 @@ _SIGS = {
     "sale_attn_fp8_operands": (ctypes.c_int, [_pp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "sale_calibrate_tau": (ctypes.c_int, [_pp, _vp, _vp, _vp, ctypes.c_float, ctypes.c_float, _i32, _vp, _vp, _vp,
                                           _vp, _sz, _vp]),
+    "sale_prompt_attn": (ctypes.c_int, [_pp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "sale_cache_append": (ctypes.c_int, [_pp, _pc, _vp, _vp, _vp]),
+    "sale_cache_copy": (ctypes.c_int, [_pp, _pc, _vp, _vp, _i32, _vp]),
+    "sale_decode_attn": (ctypes.c_int, [_pp, _pc, _vp, _vp, _i32, _vp, _vp, _vp, _sz, _vp]),
+    "sale_decode_workspace_bytes": (_sz, [_pp, _pc, _i32]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _fn = getattr(_lib, _name)
@@ -198,7 +280,7 @@ def _expect_bhnd(name: str, t, p: "Params", heads: int):
 _NO = object()
 
 
-def _args(p: "Params", q, k, v=_NO, o=_NO):
+def _args(p: "Params", q=_NO, k=_NO, v=_NO, o=_NO):
     """Checks Q, K, V, O as _expect_bhnd does -> the C struct for them, as an argument."""
     nq, nk = p._numels
     plain = True
@@ -402,3 +484,81 @@ def calibrate_tau(p: Params, q, k, v, tau0: float = 0.008, theta: float = 0.4, m
                                    _ptr(tau), _ptr(err), _ptr(halv), _ptr(ws), _expect_ws(ws),
                                    _stream()))
     return tau, err, halv
+
+
+def _on_current_device(**tensors):
+    """The calls are launched on the current device's stream."""
+    at = torch._C._cuda_getDevice()
+    for name, t in tensors.items():
+        if t is not None and t.get_device() != at:
+            raise ValueError(f"{name}: expected a tensor on the current device, cuda:{at}, got {t.device}")
+
+
+def _n_sequences(p: Params) -> int:
+    return len(p.cu_seqlens) - 1 if p.cu_seqlens else p.batch
+
+
+def prompt_attn(p: Params, q, k, v, want_lse: bool = False, out=None, ws=None):
+    """Causal attention over whole prompts of any lengths (p.seq_len, or packed ones by p.cu_seqlens; p's blocks are not read).
+    -> (o bf16 [B,Hq,N,d], lse f32 [B,Hq,N] or None)"""
+    o = torch.empty_like(q) if out is None else out
+    args = _args(p, q, k, v, o)
+    lse = torch.empty(p.batch, p.n_q_heads, p.seq_len, dtype=torch.float32, device=q.device) if want_lse else None
+    if ws is None:
+        ws = torch.empty(max(1, workspace_bytes(p, WS_PROMPT_ATTN)), dtype=torch.uint8, device=q.device)
+    _on_current_device(q=q, k=k, v=v, out=o, ws=ws)
+    _check(_lib.sale_prompt_attn(args, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(ws), _expect_ws(ws), _stream()))
+    return o, lse
+
+
+def cache_append(p: Params, cache: Cache, k, v) -> None:
+    """Writes K, V bf16 [B,Hkv,n,d] of the n = p.seq_len new tokens of every sequence (packed ones: p.cu_seqlens) into its pages,
+    as the last n of the cache.lens[s] tokens that it holds with them."""
+    c = cache._arg(p, _n_sequences(p))
+    args = _args(p, k=k, v=v)
+    _on_current_device(cache=cache.k, k=k, v=v)
+    _check(_lib.sale_cache_append(args, c, _ptr(k), _ptr(v), _stream()))
+
+
+def _host_pages(name: str, pages):
+    if not isinstance(pages, torch.Tensor):
+        pages = torch.tensor(pages, dtype=torch.int32)
+    if pages.is_cuda or pages.dtype != torch.int32 or pages.dim() != 1 or not pages.is_contiguous():
+        raise ValueError(f"{name}: expected a list of pages, or a contiguous one-dimensional int32 tensor on the host")
+    return pages
+
+
+def cache_copy(p: Params, cache: Cache, src, dst) -> None:
+    """Copies pages of K and V: dst[i] becomes src[i].  src, dst: lists or int32 tensors on the HOST; the dst all different, none
+    of them among the src."""
+    src, dst = _host_pages("src", src), _host_pages("dst", dst)
+    if src.numel() != dst.numel():
+        raise ValueError(f"cache_copy: {src.numel()} sources, {dst.numel()} destinations")
+    c = cache._arg(p)
+    _on_current_device(cache=cache.k)
+    _check(_lib.sale_cache_copy(p._contiguous, c, _ptr(src), _ptr(dst), src.numel(), _stream()))
+
+
+def decode_workspace_bytes(p: Params, cache: Cache, prefix_len: int = 0) -> int:
+    return int(_lib.sale_decode_workspace_bytes(p._contiguous, cache._arg(p, _n_sequences(p)), prefix_len))
+
+
+def decode_attn(p: Params, cache: Cache, q, prefix=None, prefix_len: int = 0, want_lse: bool = False, out=None, ws=None):
+    """Attention of the last p.seq_len tokens of every sequence, q bf16 [B,Hq,n,d], to the prefix that all share (the pages
+    `prefix`, int32 on the device, of which prefix_len tokens count) and to its own keys, the new tokens' among them.
+    -> (o bf16 [B,Hq,n,d], lse f32 [B,Hq,n] or None)"""
+    o = torch.empty_like(q) if out is None else out
+    c = cache._arg(p, _n_sequences(p))
+    args = _args(p, q, o=o)
+    if prefix_len > 0:
+        if prefix is None or prefix.dtype != torch.int32 or not prefix.is_contiguous() or \
+                prefix.numel() * cache.k.shape[2] < prefix_len:
+            raise ValueError(f"prefix: expected the pages of {prefix_len} tokens, a contiguous int32 tensor on the device")
+    else:
+        prefix = None
+    lse = torch.empty(p.batch, p.n_q_heads, p.seq_len, dtype=torch.float32, device=q.device) if want_lse else None
+    if ws is None:
+        ws = torch.empty(max(1, _lib.sale_decode_workspace_bytes(args, c, prefix_len)), dtype=torch.uint8, device=q.device)
+    _on_current_device(cache=cache.k, q=q, prefix=prefix, out=o, ws=ws)
+    _check(_lib.sale_decode_attn(args, c, _ptr(q), _ptr(prefix), prefix_len, _ptr(o), _ptr(lse), _ptr(ws), _expect_ws(ws), _stream()))
+    return o, lse

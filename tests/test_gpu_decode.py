@@ -1,0 +1,229 @@
+"""decode_attn against the oracle: heads, new tokens, page sizes and types, layouts, lengths from none, prefixes, and everything
+that is in the place of a key and is none.  Whatever is no key holds NaN here."""
+import numpy as np
+import pytest
+import torch
+
+from serving_utils import bits, check, decode_oracle, f64, make_cache, rows
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def sale():
+    from paper_2505_24179_amd import sale as mod
+    return mod
+
+
+LENS = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 130, 517]
+
+
+@pytest.mark.parametrize("hq,hkv,n,page,kind,layout,prefix_len", [
+    (4, 4, 1, 16, "bf16", "bhnd", 0), (4, 4, 1, 16, "bf16", "bnhd", 1), (6, 2, 1, 32, "bf16", "padded", 0), (6, 2, 3, 16, "fp8", "bnhd", 16),
+    (8, 2, 1, 64, "fp8", "bhnd", 0), (8, 2, 4, 64, "bf16", "bhnd", 31), (8, 2, 7, 128, "bf16", "bnhd", 33), (8, 1, 8, 256, "fp8", "padded", 300),
+    (16, 1, 1, 16, "bf16", "bhnd", 129), (34, 2, 1, 32, "fp8", "bhnd", 40), (64, 1, 1, 32, "bf16", "bhnd", 47), (5, 1, 12, 16, "bf16", "padded", 260),
+    (1, 1, 64, 64, "bf16", "bhnd", 20), (1, 1, 1, 16, "fp8", "bhnd", 15)])
+def test_against_the_oracle(sale, hq, hkv, n, page, kind, layout, prefix_len):
+    gen = torch.Generator().manual_seed(hq * 1000 + n * 10 + page)
+    cache, prefix = make_cache(sale, LENS, hkv, page, kind, layout, gen, prefix_len)
+    p = sale.Params(len(LENS), hq, hkv, n)
+    q = rows((len(LENS), hq, n, 128), layout, gen, 2.0)
+    o, lse = sale.decode_attn(p, cache, q, prefix=prefix, prefix_len=prefix_len, want_lse=True)
+    check(o, lse, decode_oracle(cache, q, prefix, prefix_len))
+    again, _ = sale.decode_attn(p, cache, q, prefix=prefix, prefix_len=prefix_len)
+    assert torch.equal(bits(again), bits(o))      # no order of anything enters the result
+
+
+@pytest.mark.parametrize("batch,longest,prefix_len,kind", [(1, 5000, 0, "bf16"), (2, 9001, 4100, "bf16"), (40, 700, 0, "fp8"), (70, 300, 2049, "bf16"),
+                                                           (300, 40, 100, "fp8")])
+def test_many_parts_and_many_rows(sale, batch, longest, prefix_len, kind):
+    """Long sequences cut over many workgroups, and batches whose rows fill several tiles of the prefix; a sample of the rows."""
+    gen = torch.Generator().manual_seed(batch + longest)
+    lens = [longest] + [int(x) for x in torch.randint(0, longest, (batch - 1,), generator=gen)]
+    cache, prefix = make_cache(sale, lens, 2, 16, kind, "bhnd", gen, prefix_len, spoil=False)
+    q = rows((batch, 8, 1, 128), "bhnd", gen, 2.0)
+    o, lse = sale.decode_attn(sale.Params(batch, 8, 2, 1), cache, q, prefix=prefix, prefix_len=prefix_len, want_lse=True)
+    some = sorted({0, batch // 3, batch - 1})
+    part = sale.Cache(cache.k, cache.v, cache.table[some].contiguous(), cache.lens[some].contiguous(), cache.k_scale, cache.v_scale)
+    check(o[some], lse[some], decode_oracle(part, q[some], prefix, prefix_len))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+def test_pages_that_are_none_and_lens_that_lie(sale, kind):
+    gen = torch.Generator().manual_seed(7)
+    cache, prefix = make_cache(sale, [100, 100, 100, 64, 40, 70], 2, 16, kind, "bhnd", gen, 50, room=0, spoil=False)
+    cache.table[0, 2], cache.table[0, 6] = -1, cache.k.shape[0]
+    cache.table[1, :] = 2 ** 31 - 1
+    cache.table[2, 0], cache.table[2, 1] = -2 ** 31, cache.k.shape[0] + 5
+    cache.lens[3], cache.lens[4], cache.lens[5] = 2 ** 31 - 1, -7, 113       # beyond the table, negative, one token beyond the table
+    prefix[1] = -3
+    q = rows((6, 8, 2, 128), "bhnd", gen, 2.0)
+    for pre in (50, 0):
+        o, lse = sale.decode_attn(sale.Params(6, 8, 2, 2), cache, q, prefix=prefix, prefix_len=pre, want_lse=True)
+        check(o, lse, decode_oracle(cache, q, prefix, pre))
+
+
+@pytest.mark.parametrize("kind,page,value", [("bf16", 16, "nan"), ("bf16", 16, "inf"), ("fp8", 64, "nan")])      # (E4M3 has no infinity)
+def test_a_new_token_does_not_reach_those_before_it(sale, kind, page, value):
+    gen = torch.Generator().manual_seed(8)
+    lens, n = [40, 65, 5, 32], 4
+    cache, prefix = make_cache(sale, lens, 2, page, kind, "bhnd", gen, 20)
+    for s, back in ((0, 1), (1, 2), (2, 3), (3, 1)):      # the last token, the one before, ...
+        pos = lens[s] - back
+        at = (int(cache.table[s, pos // page]), slice(None), pos % page)
+        if s % 2 == 0:
+            bits(cache.k)[at] = bits(torch.tensor(float(value)).to(cache.k.dtype).cuda())
+        bits(cache.v)[at + (slice(0, 128, 3),)] = bits(torch.tensor(float(value)).to(cache.v.dtype).cuda())
+    q = rows((4, 6, n, 128), "bhnd", gen)
+    o, lse = sale.decode_attn(sale.Params(4, 6, 2, n), cache, q, prefix=prefix, prefix_len=20, want_lse=True)
+    want = decode_oracle(cache, q, prefix, 20)
+    for s, back in ((0, 1), (1, 2), (2, 3), (3, 1)):
+        sound = slice(0, n - back)
+        assert torch.isfinite(o[s, :, sound]).all()
+        check(o[s:s + 1, :, sound], lse[s:s + 1, :, sound], [x[s:s + 1, :, sound] for x in want])
+        if value == "nan":
+            assert torch.isnan(o[s, :, n - back:, 0:128:3]).all()
+
+
+def test_a_query_that_is_not_finite_stays_alone(sale):
+    gen = torch.Generator().manual_seed(9)
+    cache, prefix = make_cache(sale, [50, 60, 70], 1, 16, "bf16", "bhnd", gen, 40)
+    q = rows((3, 4, 2, 128), "bhnd", gen)
+    clean, _ = sale.decode_attn(sale.Params(3, 4, 1, 2), cache, q, prefix=prefix, prefix_len=40)
+    q[1, 2, 0, 5] = float("nan")
+    q[2, 0, 1, 9] = float("inf")
+    o, _ = sale.decode_attn(sale.Params(3, 4, 1, 2), cache, q, prefix=prefix, prefix_len=40)
+    assert torch.isnan(o[1, 2, 0]).all() and torch.isnan(o[2, 0, 1]).all()
+    hit = torch.zeros(3, 4, 2, dtype=torch.bool, device="cuda")
+    hit[1, 2, 0] = hit[2, 0, 1] = True
+    assert torch.equal(o[~hit], clean[~hit])
+
+
+def test_large_values_and_scores(sale):
+    """V near the largest bf16, scores of some thousands with a maximum that rises late, equal scores."""
+    gen = torch.Generator().manual_seed(10)
+    cache, _ = make_cache(sale, [700, 700, 700], 1, 16, "bf16", "bhnd", gen, spoil=False)
+    n_pages = cache.k.shape[0]
+    cache.v.mul_(0).add_(3.2e38)
+    cache.k.mul_(torch.linspace(0.1, 60.0, n_pages, device="cuda")[:, None, None, None].bfloat16())
+    q = rows((3, 4, 1, 128), "bhnd", gen, 3.0)
+    q[1] *= 1e-30
+    o, lse = sale.decode_attn(sale.Params(3, 4, 1, 1), cache, q, want_lse=True)
+    check(o, lse, decode_oracle(cache, q, None, 0))
+    assert torch.isfinite(o).all()
+
+
+def test_nothing_beyond_the_outputs_is_written(sale):
+    gen = torch.Generator().manual_seed(11)
+    cache, prefix = make_cache(sale, [33, 0, 90], 2, 16, "bf16", "bhnd", gen, 35)
+    p = sale.Params(3, 6, 2, 3)
+    q = rows((3, 6, 3, 128), "bhnd", gen)
+    plain, _ = sale.decode_attn(p, cache, q, prefix=prefix, prefix_len=35)
+    before = bits(cache.k).clone(), bits(cache.v).clone()
+    big = torch.full((4, 8, 5, 160), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = big[:3, 1:7, 1:4, 16:144]
+    need = sale.decode_workspace_bytes(p, cache, 35)
+    ws = torch.full((need + 4096,), 173, dtype=torch.uint8, device="cuda")
+    sale.decode_attn(p, cache, q, prefix=prefix, prefix_len=35, out=out, ws=ws[:need])
+    assert torch.equal(out, plain) and bool((ws[need:] == 173).all())
+    out.fill_(7.0)
+    assert bool((big == 7.0).all())
+    assert torch.equal(bits(cache.k), before[0]) and torch.equal(bits(cache.v), before[1])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+def test_offsets_beyond_32_bits(sale, kind):
+    """Pages at the far end of pools of more than 4 GB each."""
+    gen = torch.Generator().manual_seed(12)
+    size = 2 if kind == "bf16" else 1
+    n_pages = (5 << 30) // (128 * 128 * 8 * size)
+    small, _ = make_cache(sale, [300], 8, 128, kind, "bhnd", gen, spoil=False)
+    far = [n_pages - 1, 3, n_pages - 4]
+    k = torch.empty(n_pages, 8, 128, 128, dtype=torch.uint8 if size == 1 else torch.int16, device="cuda")
+    v = torch.empty_like(k)
+    for i, at in enumerate(far):
+        k[at], v[at] = bits(small.k)[int(small.table[0, i])], bits(small.v)[int(small.table[0, i])]
+    big = sale.Cache(k.view(small.k.dtype), v.view(small.v.dtype), torch.tensor([far], dtype=torch.int32, device="cuda"), small.lens,
+                     small.k_scale, small.v_scale)
+    q = rows((1, 8, 1, 128), "bhnd", gen)
+    near = sale.Cache(small.k, small.v, small.table[:, :3].contiguous(), small.lens, small.k_scale, small.v_scale)
+    p = sale.Params(1, 8, 8, 1)
+    assert torch.equal(sale.decode_attn(p, big, q)[0], sale.decode_attn(p, near, q)[0])
+
+
+def test_captured_with_lens_that_grow(sale):
+    """Captured once; lens, table, queries and pages change between the replays.  Two graphs with workspaces of their own."""
+    gen = torch.Generator().manual_seed(13)
+    lens = [0, 17, 60, 250]
+    cache, prefix = make_cache(sale, lens, 2, 16, "bf16", "bhnd", gen, 77, room=3, spoil=False)
+    p = sale.Params(4, 8, 2, 1)
+    q, new = rows((4, 8, 1, 128), "bhnd", gen), rows((4, 2, 1, 128), "bhnd", gen)
+    free = [i for i in range(cache.k.shape[0]) if i not in set(cache.table.flatten().tolist()) | set(prefix.tolist())]
+    cache.table[0, 0], cache.table[2, 4] = free[0], free[1]      # (room for the tokens to come)
+    o = torch.empty_like(q)
+    ws = torch.empty(sale.decode_workspace_bytes(p, cache, 77), dtype=torch.uint8, device="cuda")
+
+    def step():
+        cache.lens.add_(1)
+        sale.cache_append(p, cache, new, new)
+        sale.decode_attn(p, cache, q, prefix=prefix, prefix_len=77, out=o, ws=ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+        cache.lens.sub_(1)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for replay in range(5):
+        q.copy_(rows((4, 8, 1, 128), "bhnd", gen))
+        new.copy_(rows((4, 2, 1, 128), "bhnd", gen))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert cache.lens.tolist() == [n + 1 + replay for n in lens]
+        eager, _ = sale.decode_attn(p, cache, q, prefix=prefix, prefix_len=77)
+        assert torch.equal(eager, o)
+        for s in range(4):
+            pos = lens[s] + replay
+            page = int(cache.table[s, pos // 16])
+            assert torch.equal(cache.k[page, :, pos % 16], new[s, :, 0])
+
+
+def test_on_another_stream(sale):
+    gen = torch.Generator().manual_seed(14)
+    cache, prefix = make_cache(sale, [900, 20], 2, 32, "bf16", "bhnd", gen, 64, spoil=False)
+    p, q = sale.Params(2, 8, 2, 1), rows((2, 8, 1, 128), "bhnd", gen)
+    want, _ = sale.decode_attn(p, cache, q, prefix=prefix, prefix_len=64)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        late = q * 0
+        late += q
+        got, _ = sale.decode_attn(p, cache, late, prefix=prefix, prefix_len=64)
+    side.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_what_the_binding_refuses(sale):
+    gen = torch.Generator().manual_seed(15)
+    cache, prefix = make_cache(sale, [30, 20], 2, 16, "bf16", "bhnd", gen, 64)
+    q = rows((2, 8, 1, 128), "bhnd", gen)
+    p = sale.Params(2, 8, 2, 1)
+    for args, kw in (((sale.Params(3, 8, 2, 1), cache, q), {}), ((sale.Params(2, 8, 4, 1), cache, q), {}), ((p, cache, q.float()), {}),
+                     ((p, cache, q[:, :4]), {}), ((p, cache, q.cpu()), {}), ((p, cache, q), dict(prefix_len=10)),
+                     ((p, cache, q), dict(prefix=prefix, prefix_len=65)), ((p, cache, q), dict(prefix=prefix.long(), prefix_len=64)),
+                     ((p, cache, q), dict(prefix=prefix.cpu(), prefix_len=64)), ((p, cache, q), dict(out=q[:, :, :, :64])),
+                     ((p, cache, q), dict(ws=torch.empty(10)))):
+        with pytest.raises(ValueError):
+            sale.decode_attn(*args, **kw)
+    with pytest.raises(sale.SaleError):
+        sale.decode_attn(p, cache, q, prefix=prefix, prefix_len=64, ws=torch.empty(10, device="cuda"))
+    k, v, t, n = cache.k, cache.v, cache.table, cache.lens
+    for args in ((k.float(), v.float(), t, n), (k, v[:1], t, n), (k, v, t.long(), n), (k, v, t, n[:1]), (k, v, t[0], n), (k, v, t.cpu(), n),
+                 (k.transpose(2, 3), v.transpose(2, 3), t, n), (bits(k).view(torch.float8_e4m3fn)[..., :128], bits(v).view(torch.float8_e4m3fn)[..., :128], t, n)):
+        with pytest.raises(ValueError):
+            sale.Cache(*args)

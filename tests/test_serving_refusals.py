@@ -1,0 +1,147 @@
+"""What the serving calls refuse, before anything is launched: through the C ABI with pointers that are never followed, and in
+the binding's own checks."""
+import ctypes
+
+import pytest
+import torch
+
+F = ctypes.c_void_p(0x1000)
+
+
+@pytest.fixture(scope="module")
+def sale():
+    from paper_2505_24179_amd import sale as mod
+    return mod
+
+
+def _cache(sale, **kw):
+    c = sale._Cache(k=0x1000, v=0x1000, n_pages=10, page_tokens=16, dtype=0, table_width=4, table=0x1000, lens=0x1000)
+    for name, x in kw.items():
+        if name.endswith("stride"):
+            getattr(c, name)[:] = x
+        else:
+            setattr(c, name, x)
+    return c
+
+
+def _params(sale, batch=2, hq=8, hkv=2, n=1, **kw):
+    p = sale.Params(batch, hq, hkv, n, **{k: v for k, v in kw.items() if not k.endswith("_stride")})
+    c = p.c()
+    for name in kw:
+        if name.endswith("_stride"):
+            getattr(c, name)[:] = kw[name]
+    return c
+
+
+BAD_PARAMS = [(dict(batch=0), -2), (dict(n=0), -2), (dict(n=-1), -2), (dict(hq=7), -2), (dict(hkv=0), -2), (dict(head_dim=64), -3),
+              (dict(flags=8), -3), (dict(flags=32), -3), (dict(cu_seqlens=(0, 1)), -2), (dict(batch=1, n=3, cu_seqlens=(0, 2, 1, 3)), -2),
+              (dict(batch=1, n=3, cu_seqlens=(0, 2)), -2), (dict(batch=1, n=3, cu_seqlens=(1, 3)), -2)]
+
+
+@pytest.mark.parametrize("kw,status", BAD_PARAMS)
+def test_parameters(sale, kw, status):
+    lib, p, c = sale.raw(), _params(sale, **kw), _cache(sale)
+    b = ctypes.byref
+    assert lib.sale_prompt_attn(b(p), F, F, F, F, None, F, 1 << 40, None) == status
+    assert lib.sale_workspace_bytes(b(p), sale.WS_PROMPT_ATTN) == 0
+    assert lib.sale_cache_append(b(p), b(c), F, F, None) == status
+    assert lib.sale_decode_attn(b(p), b(c), F, None, 0, F, None, F, 1 << 40, None) == status
+    assert lib.sale_decode_workspace_bytes(b(p), b(c), 0) == 0
+
+
+@pytest.mark.parametrize("stride", [(128, 64, 4), (0, 128, 128), (1024, 0, 128), (1024, 128, 64), (1024, 129, 128), (1024, -128, 128)])
+def test_strides(sale, stride):
+    lib, c, b = sale.raw(), _cache(sale), ctypes.byref
+    p = _params(sale, q_stride=stride)
+    assert lib.sale_prompt_attn(b(p), F, F, F, F, None, F, 1 << 40, None) == -2
+    assert lib.sale_decode_attn(b(p), b(c), F, None, 0, F, None, F, 1 << 40, None) == -2
+    p = _params(sale, k_stride=stride)
+    assert lib.sale_cache_append(b(p), b(c), F, F, None) == -2
+
+
+BAD_CACHE = [(dict(k=None), -1), (dict(v=None), -1), (dict(table=None), -1), (dict(lens=None), -1), (dict(n_pages=0), -2),
+             (dict(table_width=0), -2), (dict(page_tokens=0), -2), (dict(page_tokens=8), -3), (dict(page_tokens=48), -3),
+             (dict(page_tokens=512), -3), (dict(dtype=2), -3), (dict(dtype=1), -1), (dict(dtype=1, k_scale=0x1000), -1),
+             (dict(k=0x1008), -2), (dict(v=0x1002), -2), (dict(k_stride=(4096, 2048, 64)), -2), (dict(v_stride=(4096, 2048, 132)), -2),
+             (dict(k_stride=(4096, 0, 128)), -2), (dict(v_stride=(0, 2048, 128)), -2), (dict(k_stride=(4096, 2048, 1 << 25)), -2),
+             (dict(k_stride=(-4096, 2048, 128)), -2), (dict(dtype=1, k_scale=0x1000, v_scale=0x1000, k_stride=(4096, 2048, 136)), -2),
+             (dict(table_width=1 << 28), -3)]
+
+
+@pytest.mark.parametrize("kw,status", BAD_CACHE)
+def test_caches(sale, kw, status):
+    lib, p, c, b = sale.raw(), _params(sale), _cache(sale, **kw), ctypes.byref
+    assert lib.sale_cache_append(b(p), b(c), F, F, None) == status
+    assert lib.sale_decode_attn(b(p), b(c), F, None, 0, F, None, F, 1 << 40, None) == status
+    assert lib.sale_decode_workspace_bytes(b(p), b(c), 0) == 0
+
+
+def test_null_and_misaligned_tensors(sale):
+    lib, p, c, b = sale.raw(), _params(sale), _cache(sale), ctypes.byref
+    odd = ctypes.c_void_p(0x1004)
+    for at in range(4):
+        args = [F, F, F, F]
+        args[at] = None
+        assert lib.sale_prompt_attn(b(p), *args, None, F, 1 << 40, None) == -1
+        args[at] = odd
+        assert lib.sale_prompt_attn(b(p), *args, None, F, 1 << 40, None) == -2
+    assert lib.sale_cache_append(b(p), b(c), None, F, None) == -1 and lib.sale_cache_append(b(p), b(c), F, odd, None) == -2
+    assert lib.sale_cache_append(b(p), None, F, F, None) == -1 and lib.sale_cache_append(None, b(c), F, F, None) == -1
+    assert lib.sale_decode_attn(b(p), b(c), None, None, 0, F, None, F, 1 << 40, None) == -1
+    assert lib.sale_decode_attn(b(p), b(c), F, None, 0, None, None, F, 1 << 40, None) == -1
+    assert lib.sale_decode_attn(b(p), b(c), F, None, 5, F, None, F, 1 << 40, None) == -1      # a prefix without its pages
+    assert lib.sale_decode_attn(b(p), b(c), F, F, -1, F, None, F, 1 << 40, None) == -2
+    assert lib.sale_decode_attn(b(p), b(c), odd, None, 0, F, None, F, 1 << 40, None) == -2
+
+
+def test_sizes_that_are_not_supported(sale):
+    lib, c, b = sale.raw(), _cache(sale), ctypes.byref
+    decode = lambda p, prefix=0: lib.sale_decode_attn(b(p), b(c), F, F, prefix, F, None, F, 1 << 40, None)
+    assert decode(_params(sale, hq=64, hkv=1, n=2)) == -3             # 128 rows for one KV head
+    assert decode(_params(sale, n=17)) == -3
+    assert decode(_params(sale, batch=1, n=2, cu_seqlens=(0, 1, 2))) == -3
+    assert decode(_params(sale), 1 << 30) == -3
+    assert decode(_params(sale, batch=1 << 30)) == -3
+    assert lib.sale_prompt_attn(b(_params(sale, batch=1, n=262145)), F, F, F, F, None, F, 1 << 60, None) == -3
+    assert lib.sale_workspace_bytes(b(_params(sale, batch=1, n=262144)), sale.WS_PROMPT_ATTN) > 0
+    assert lib.sale_prompt_attn(b(_params(sale, batch=1 << 20, n=262144)), F, F, F, F, None, F, 1 << 60, None) == -3
+
+
+def test_workspaces(sale):
+    lib, c, b = sale.raw(), _cache(sale), ctypes.byref
+    p = _params(sale, n=100)
+    need = lib.sale_workspace_bytes(b(p), sale.WS_PROMPT_ATTN)
+    assert need >= 2 * 2 * 2 * 128 * 256      # K' and V' of two batch entries, two heads, two blocks
+    for ws, size in ((None, need), (F, need - 1), (ctypes.c_void_p(0x1008), need)):
+        assert lib.sale_prompt_attn(b(p), F, F, F, F, None, ws, size, None) == -4
+    p = _params(sale)
+    need = lib.sale_decode_workspace_bytes(b(p), b(c), 40)
+    assert need > 0 and lib.sale_decode_workspace_bytes(b(p), b(c), 0) < need
+    for ws, size in ((None, need), (F, need - 1), (ctypes.c_void_p(0x1008), need)):
+        assert lib.sale_decode_attn(b(p), b(c), F, F, 40, F, None, ws, size, None) == -4
+
+
+@pytest.mark.parametrize("src,dst", [([0], [0]), ([0, 1], [2, 2]), ([0, 1], [1, 2]), ([0, 1], [2, 0]), ([10], [1]), ([1], [10]),
+                                     ([-1], [1]), ([1], [-1]), ([0, 0, 0], [1, 2, 1])])
+def test_copies_that_overlap(sale, src, dst):
+    lib, p, c, b = sale.raw(), _params(sale), _cache(sale, table=None, lens=None), ctypes.byref
+    i32 = ctypes.c_int32 * len(src)
+    assert lib.sale_cache_copy(b(p), b(c), i32(*src), i32(*dst), len(src), None) == -2
+
+
+def test_copies(sale):
+    lib, p, c, b = sale.raw(), _params(sale), _cache(sale), ctypes.byref
+    one = (ctypes.c_int32 * 1)(1)
+    assert lib.sale_cache_copy(b(p), b(c), None, None, 0, None) == 0      # nothing to do, nothing launched
+    assert lib.sale_cache_copy(b(p), b(c), None, one, 1, None) == -1
+    assert lib.sale_cache_copy(b(p), b(c), one, one, -1, None) == -2
+    assert lib.sale_cache_copy(b(_params(sale, head_dim=64)), b(c), one, one, 1, None) == -3
+    assert lib.sale_cache_copy(b(_params(sale, hq=1 << 30, hkv=1 << 30)), b(_cache(sale, page_tokens=256)), one, (ctypes.c_int32 * 1)(2), 1, None) == -3
+
+
+def test_the_binding_takes_device_tensors_only(sale):
+    k = torch.zeros(4, 2, 16, 128, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="device tensor"):
+        sale.Cache(k, k, torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32))
+    with pytest.raises(ValueError, match="device tensor"):
+        sale.prompt_attn(sale.Params(1, 2, 2, 5), *(torch.zeros(1, 2, 5, 128, dtype=torch.bfloat16) for _ in range(3)))
