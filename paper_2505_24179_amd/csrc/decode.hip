@@ -40,10 +40,13 @@ struct DecodeArgs {
   Strided sq, so;
   const int32_t* prefix_table;
   int prefix_len, n_seqs, n_new, group, n_kvh;
-  int own_parts, own_least;                     // parts of a sequence's own keys, and the fewest keys that one of them takes
+  int shares;                                   // workgroups per KV head for the own keys
   int prefix_parts, prefix_chunk, row_tiles;    // parts of the prefix, keys of each; tiles of 16 * (row tiles of the kernel) rows
-  f32x4* own_acc;  float2* own_sum;             // [sequence][KV head][part] partial results: [row tile][8][64], [row]
-  f32x4* pre_acc;  float2* pre_sum;             // [tile][KV head][part]
+  // Partial results, by slot: accumulators [8][4 (g)][row], sums [row].  Own keys: share j of sequence s in slot j + s of the KV
+  // head's (from one piece to the next j or s or both go up by one); prefix: [tile][KV head][part].
+  f32x4 *own_acc, *pre_acc;
+  float2 *own_sum, *pre_sum;
+  int2* turns;                                  // [KV head][sequence] first turn of a sequence that has one, and those of all
 };
 
 // Channels of a lane's Q operand of contraction step s: those that its K operand has.
@@ -266,8 +269,8 @@ __device__ __forceinline__ void sweep(const CacheView& c, const Keys& ks, int kv
   }
 }
 
-// The results of the four waves, joined: sum (one per row) and acc (one 16-row tile after the other, 8 x 64 lanes x 4 floats).
-// keep(qt, c, x): x = accumulator c of this lane in tile qt, for two numbers c per wave; sums(row, ref, l).
+// The results of the four waves, joined.  keep(qt, c, x, l): x = accumulator c of this lane in tile qt, l the sum of its row, for
+// two numbers c per wave; sums(row, ref, l).
 struct JoinLds {
   f32x4 acc[kWaves][8][64];
   float ref[kWaves][64], l[kWaves][64];
@@ -314,10 +317,14 @@ __device__ __forceinline__ float lse_of(float ref, float l) { return l == 0.0f ?
 struct RowOf { int token, head; };
 __device__ __forceinline__ RowOf row_of(const DecodeArgs& a, int r) { const int t = r / a.group; return {t, r - t * a.group}; }
 
+__device__ __forceinline__ uint16_t* row_at(uint16_t* x, const Strided& l, int s, int head, int token) {
+  return x + (size_t)s * (size_t)l.sb + (size_t)head * (size_t)l.sh + (size_t)token * (size_t)l.st;
+}
+
 template <bool FP8, int NT>
 __device__ __forceinline__ void load_row(const DecodeArgs& a, int kvh, int s, int r, int qt, int g, Rows<FP8, NT>& rows) {
   const RowOf w = row_of(a, r);
-  const uint16_t* row = a.q + row_off(a.sq, s * a.sq.heads + kvh * a.group + w.head, w.token);
+  const uint16_t* row = row_at(const_cast<uint16_t*>(a.q), a.sq, s, kvh * a.group + w.head, w.token);
 #pragma unroll
   for (int e = 0; e < 4; ++e) rows.q[qt][e] = *(const bf16x8*)(row + step_channel<FP8>(e, g));
   rows.token[qt] = w.token;
@@ -327,50 +334,82 @@ __device__ __forceinline__ void load_row(const DecodeArgs& a, int kvh, int s, in
   for (int c = 0; c < 8; ++c) rows.acc[qt][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 }
 
-// A workgroup: one part of a sequence's own keys, for the rows of one KV head.
-template <bool FP8, int NT, bool DIRECT>
+// Sharing out the own keys.  A sequence has as many turns as workgroups need to read its keys, kTurn at a time; the turns of
+// all sequences, one after the other, are dealt to the workgroups of a KV head in equal shares.
+__device__ __forceinline__ int keys_of(const CacheView& c, int s) { return min(max(c.lens[s], 0), c.width << c.page_shift); }
+__device__ __forceinline__ int turns_of(const CacheView& c, int s) { return (keys_of(c, s) + kTurn - 1) / kTurn; }
+struct Share { long long first, count; };
+__device__ __forceinline__ Share share_of(long long turns, int shares, int j) {
+  const long long each = turns / shares, more = turns - each * shares;      // (the first `more` shares have one turn more)
+  return {j * each + min((long long)j, more), each + (j < more ? 1 : 0)};
+}
+__device__ __forceinline__ int share_with(long long turns, int shares, long long turn) {
+  const long long each = turns / shares, more = turns - each * shares, border = more * (each + 1);
+  return (int)(turn < border ? turn / (each + 1) : more + (turn - border) / each);
+}
+
+// A workgroup: one share of the turns of a KV head, piece by piece (a piece: neighbouring turns of one sequence).  The only piece
+// of a sequence, without a prefix, is its result.
+template <bool FP8, int NT>
 __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void own_kernel(DecodeArgs a) {
   __shared__ JoinLds lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, g = lane >> 4, n_rows = a.group * a.n_new;
-  const int kvh = blockIdx.x % a.n_kvh, rest = blockIdx.x / a.n_kvh, part = rest % a.own_parts, s = rest / a.own_parts;
-  const size_t slot = ((size_t)s * a.n_kvh + kvh) * a.own_parts + part;
-  const int held = max(a.c.lens[s], 0), n_keys = min(held, a.c.width << a.c.page_shift);
-  const int chunk = max(a.own_least, ((n_keys + a.own_parts - 1) / a.own_parts + kTurn - 1) / kTurn * kTurn);
-  const int lo = (int)min((long long)part * chunk, (long long)n_keys), hi = min(lo + chunk, n_keys);
-  if (!DIRECT && lo >= hi) {
-    if (tid < 16 * NT) a.own_sum[slot * 16 * NT + tid] = make_float2(kNoRef, 0.0f);
-    return;
-  }
-  Rows<FP8, NT> rows;
+  const int kvh = blockIdx.x % a.n_kvh, j = blockIdx.x / a.n_kvh;
+  // lane i counts the turns of sequences i * per ..
+  const int per = (a.n_seqs + 63) / 64;
+  int mine = 0;
+  for (int s = lane * per; s < min((lane + 1) * per, a.n_seqs); ++s) mine += turns_of(a.c, s);
+  int upto = mine;
 #pragma unroll
-  for (int qt = 0; qt < NT; ++qt) load_row<FP8, NT>(a, kvh, s, min(16 * qt + n, n_rows - 1), qt, g, rows);
-  const Keys ks = {a.c.table + (size_t)s * a.c.width, n_keys, min(held - a.n_new + 1, n_keys), held - a.n_new};
-  const float scale = FP8 ? kLog2eByRootD * a.c.k_scale[kvh] : kLog2eByRootD;
-  sweep<FP8, NT>(a.c, ks, kvh, lo, hi, wave, lane, a.n_new, scale, rows);
-  const float v_scale = FP8 ? a.c.v_scale[kvh] : 1.0f;
-  join_waves<FP8, NT>(rows, lds, wave, lane,
-    [&](int qt, int c, f32x4 x, float l) {
-      if constexpr (DIRECT) {
+  for (int d = 1; d < 64; d *= 2) { const int x = __shfl_up(upto, d, 64); if (lane >= d) upto += x; }
+  const int all = __builtin_amdgcn_readlane(upto, 63);
+  const Share share = share_of(all, a.shares, j);
+  if (share.count == 0) return;
+  const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > share.first));
+  int s = at * per, base = __builtin_amdgcn_readlane(upto - mine, at), left = (int)share.count;      // base: first turn of sequence s
+  const float scale = FP8 ? kLog2eByRootD * a.c.k_scale[kvh] : kLog2eByRootD, v_scale = FP8 ? a.c.v_scale[kvh] : 1.0f;
+  int turn = (int)share.first;
+  for (; left > 0; ++s) {
+    const int held = max(a.c.lens[s], 0), n_keys = keys_of(a.c, s), turns = (n_keys + kTurn - 1) / kTurn;
+    if (turn >= base + turns) { base += turns; continue; }
+    const int from = turn - base, count = min(turns - from, left);
+    const int lo = from * kTurn, hi = min((from + count) * kTurn, n_keys);
+    const bool whole = count == turns && a.prefix_len == 0;
+    const size_t slot = (size_t)kvh * (a.shares + a.n_seqs) + j + s;
+    if (from == 0 && tid == 0) a.turns[(size_t)kvh * a.n_seqs + s] = make_int2(base, all);
+    Rows<FP8, NT> rows;
+#pragma unroll
+    for (int qt = 0; qt < NT; ++qt) load_row<FP8, NT>(a, kvh, s, min(16 * qt + n, n_rows - 1), qt, g, rows);
+    const Keys ks = {a.c.table + (size_t)s * a.c.width, n_keys, min(held - a.n_new + 1, n_keys), held - a.n_new};
+    sweep<FP8, NT>(a.c, ks, kvh, lo, hi, wave, lane, a.n_new, scale, rows);
+    join_waves<FP8, NT>(rows, lds, wave, lane,
+      [&](int qt, int c, f32x4 x, float l) {
         const int r = 16 * qt + n;
         if (r >= n_rows) return;
-        const RowOf w = row_of(a, r);
-        uint16_t* out = a.o + row_off(a.so, s * a.so.heads + kvh * a.group + w.head, w.token) + 32 * g + c;
+        if (whole) {
+          const RowOf w = row_of(a, r);
+          uint16_t* out = row_at(a.o, a.so, s, kvh * a.group + w.head, w.token) + 32 * g + c;
+          const float by = l == 0.0f ? 0.0f : v_scale / l;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) out[8 * e] = __builtin_bit_cast(uint16_t, (__bf16)(l == 0.0f ? 0.0f : x[e] / l * v_scale));
-      } else {
-        a.own_acc[((slot * NT + qt) * 8 + c) * 64 + lane] = x;
-      }
-    },
-    [&](int row, float ref, float l) {
-      if constexpr (DIRECT) {
-        if (row >= n_rows || !a.lse) return;
-        const RowOf w = row_of(a, row);
-        a.lse[((size_t)s * a.sq.heads + kvh * a.group + w.head) * a.n_new + w.token] = lse_of(ref, l);
-      } else {
-        a.own_sum[slot * 16 * NT + row] = make_float2(ref, l);
-      }
-    });
+          for (int e = 0; e < 4; ++e) out[8 * e] = __builtin_bit_cast(uint16_t, (__bf16)(l == 0.0f ? 0.0f : x[e] * by));
+        } else {
+          a.own_acc[((slot * 8 + c) * 4 + g) * n_rows + r] = x;
+        }
+      },
+      [&](int r, float ref, float l) {
+        if (r >= n_rows) return;
+        if (whole) {
+          const RowOf w = row_of(a, r);
+          if (a.lse) a.lse[((size_t)s * a.sq.heads + kvh * a.group + w.head) * a.n_new + w.token] = lse_of(ref, l);
+        } else {
+          a.own_sum[slot * n_rows + r] = make_float2(ref, l);
+        }
+      });
+    left -= count;
+    turn += count;
+    base += turns;
+  }
 }
 
 // A workgroup: one part of the prefix, for 16 NT rows of one KV head, of whichever sequences.
@@ -393,43 +432,88 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void prefix_kernel(De
   const float scale = FP8 ? kLog2eByRootD * a.c.k_scale[kvh] : kLog2eByRootD;
   sweep<FP8, NT>(a.c, ks, kvh, lo, hi, wave, lane, 1, scale, rows);
   join_waves<FP8, NT>(rows, lds, wave, lane,
-    [&](int qt, int c, f32x4 x, float) { a.pre_acc[((slot * NT + qt) * 8 + c) * 64 + lane] = x; },
+    [&](int qt, int c, f32x4 x, float) { a.pre_acc[((slot * 8 + c) * 4 + g) * (16 * NT) + 16 * qt + n] = x; },
     [&](int row, float ref, float l) { a.pre_sum[slot * 16 * NT + row] = make_float2(ref, l); });
 }
 
-// Joins the parts of 16 rows of a sequence and KV head.  Wave c has the accumulators of number c; the rows leave through LDS as
-// whole ones.
-__global__ __launch_bounds__(512) void join_kernel(DecodeArgs a, int own_tiles, int pre_tiles) {
+// Joins the parts of 16 rows of a sequence and KV head.  The weights of the parts first, kMostWeights at a time, in LDS; then wave
+// (half, c) adds up the accumulators of number c of every other part, 4 loads in flight; the rows leave through LDS as whole ones.
+constexpr int kMostWeights = 256;
+__global__ __launch_bounds__(1024) void join_kernel(DecodeArgs a, int pre_rows) {
   __shared__ __attribute__((aligned(16))) uint16_t out[16][kHeadDim + 8];
-  const int tid = threadIdx.x, lane = tid & 63, c = __builtin_amdgcn_readfirstlane(tid >> 6);
+  __shared__ float weight[kMostWeights][16], most[64][16], sums[64][16];
+  __shared__ f32x4 half_acc[8][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = wave & 7, half = wave >> 3;
   const int n = lane & 15, g = lane >> 4, n_rows = a.group * a.n_new;
-  const int kvh = blockIdx.x % a.n_kvh, rest = blockIdx.x / a.n_kvh, qt = rest % own_tiles, s = rest / own_tiles;
+  const int kvh = blockIdx.x % a.n_kvh, rest = blockIdx.x / a.n_kvh, tiles = (n_rows + 15) / 16, qt = rest % tiles, s = rest / tiles;
   const int r = min(16 * qt + n, n_rows - 1);
-  const size_t own = ((size_t)s * a.n_kvh + kvh) * a.own_parts;
-  const int row = s * n_rows + r, tile = row / (16 * pre_tiles), in_tile = row - tile * 16 * pre_tiles;
+  const int turns = turns_of(a.c, s);
+  int own_parts = 0;
+  size_t own = 0;      // slot of the first part of the own keys
+  if (turns > 0) {
+    const int2 at = a.turns[(size_t)kvh * a.n_seqs + s];
+    const int first = share_with(at.y, a.shares, at.x);
+    own_parts = share_with(at.y, a.shares, at.x + turns - 1) - first + 1;
+    own = (size_t)kvh * (a.shares + a.n_seqs) + first + s;
+    if (own_parts == 1 && a.prefix_len == 0) return;      // (already the result)
+  }
+  const int row = s * n_rows + r, tile = row / pre_rows, in_tile = row - tile * pre_rows;
   const size_t pre = ((size_t)tile * a.n_kvh + kvh) * a.prefix_parts;
+  const int parts = a.prefix_parts + own_parts;
+  // part i of this lane's row: the prefix's first
+  auto sum_of = [&](int i) {
+    return i < a.prefix_parts ? a.pre_sum[(pre + i) * pre_rows + in_tile] : a.own_sum[(own + i - a.prefix_parts) * n_rows + r];
+  };
+  const int seat = tid >> 4;      // 64 parts at a time, 16 rows each (tid % 16 = n)
   float top = kNoRef;
-  for (int i = 0; i < a.prefix_parts; ++i) top = fmaxf(top, a.pre_sum[(pre + i) * 16 * pre_tiles + in_tile].x);
-  for (int i = 0; i < a.own_parts; ++i) top = fmaxf(top, a.own_sum[(own + i) * 16 * own_tiles + r].x);
+  for (int i = seat; i < parts; i += 64) top = fmaxf(top, sum_of(i).x);
+  most[seat][n] = top;
+  __syncthreads();
+  for (int i = 0; i < min(64, parts); ++i) top = fmaxf(top, most[i][n]);
   float l = 0.0f;
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  auto add = [&](float2 sum, const f32x4* from) {
-    if (sum.y == 0.0f) return;      // (a part without keys for this row: its accumulators may not be there)
-    const float by = __builtin_amdgcn_exp2f(sum.x - top);
-    l += by * sum.y;
-    acc += by * *from;
-  };
-  for (int i = 0; i < a.prefix_parts; ++i)
-    add(a.pre_sum[(pre + i) * 16 * pre_tiles + in_tile],
-        a.pre_acc + (((pre + i) * pre_tiles + in_tile / 16) * 8 + c) * 64 + 16 * g + in_tile % 16);
-  for (int i = 0; i < a.own_parts; ++i)
-    add(a.own_sum[(own + i) * 16 * own_tiles + r], a.own_acc + (((own + i) * own_tiles + qt) * 8 + c) * 64 + 16 * g + r % 16);
-  const float by = l == 0.0f ? 0.0f : (a.c.v_scale ? a.c.v_scale[kvh] : 1.0f) / l;
+  for (int i0 = 0; i0 < parts; i0 += kMostWeights) {
+    const int here = min(kMostWeights, parts - i0);
+    if (i0 > 0) __syncthreads();
+    for (int i = seat; i < (here + 7 & ~7); i += 64) {
+      const float2 x = i < here ? sum_of(i0 + i) : make_float2(0.0f, 0.0f);
+      // (a part without keys for this row has no accumulators)
+      const float w = x.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(x.x - top);
+      weight[i][n] = w;
+      if (x.y != 0.0f) l += w * x.y;
+    }
+    __syncthreads();
+    for (int i = half; i < here; i += 8) {
+      f32x4 x[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) out[n][32 * g + 8 * e + c] = __builtin_bit_cast(uint16_t, (__bf16)(l == 0.0f ? 0.0f : acc[e] * by));
-  if (a.lse && c == 0 && g == 0 && 16 * qt + n < n_rows) {
-    const RowOf w = row_of(a, r);
-    a.lse[((size_t)s * a.sq.heads + kvh * a.group + w.head) * a.n_new + w.token] = lse_of(top, l);
+      for (int e = 0; e < 4; ++e) {
+        const int at = min(i0 + i + 2 * e, parts - 1), mine = at - a.prefix_parts;
+        const f32x4* from = mine < 0 ? a.pre_acc + (((pre + at) * 8 + c) * 4 + g) * pre_rows + in_tile
+                                     : a.own_acc + (((own + mine) * 8 + c) * 4 + g) * n_rows + r;
+        x[e] = *from;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float w = weight[i + 2 * e][n];
+#pragma unroll
+        for (int f = 0; f < 4; ++f) acc[f] += w == 0.0f ? 0.0f : w * x[e][f];
+      }
+    }
+  }
+  sums[seat][n] = l;
+  if (half == 1) half_acc[c][lane] = acc;
+  __syncthreads();
+  if (half == 0) {
+    l = 0.0f;
+    for (int i = 0; i < min(64, parts); ++i) l += sums[i][n];
+    acc += half_acc[c][lane];
+    const float by = l == 0.0f ? 0.0f : (a.c.v_scale ? a.c.v_scale[kvh] : 1.0f) / l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[n][32 * g + 8 * e + c] = __builtin_bit_cast(uint16_t, (__bf16)(l == 0.0f ? 0.0f : acc[e] * by));
+    if (a.lse && c == 0 && g == 0 && 16 * qt + n < n_rows) {
+      const RowOf w = row_of(a, r);
+      a.lse[((size_t)s * a.sq.heads + kvh * a.group + w.head) * a.n_new + w.token] = lse_of(top, l);
+    }
   }
   __syncthreads();
   const int line = tid >> 4, r_out = 16 * qt + line;
@@ -441,43 +525,45 @@ __global__ __launch_bounds__(512) void join_kernel(DecodeArgs a, int own_tiles, 
 }
 
 // How a call is cut, from its sizes alone.
+// kShares: workgroups that a call's own keys, and the parts of its prefix, are dealt to: two per CU.  64 sequences of 0 .. 8000
+// keys, page by page: 205.8 us with 256, 207.4 with 512, 208.1 with 1024, 210.9 with 2048, 217.8 with 4096; 4 sequences of 65000 ..
+// 131072 keys: 266.8, 263.6, 268.9, 275.7, 291.9.  (More of them only read and write more partial results.  Cut into a number of
+// parts that each sequence had to itself, the first took 251 us: the longest sequences' parts ended last.)
+constexpr int kShares = 512;
 struct Plan {
   int own_tiles, pre_tiles;      // 16-row tiles per workgroup
-  int own_parts, own_least, prefix_parts, prefix_chunk, row_tiles;
-  bool direct;                   // one part: the result itself
-  size_t own_slots, pre_slots;
-  size_t own_acc_bytes, own_sum_bytes, pre_acc_bytes, pre_sum_bytes, bytes;
+  int shares, prefix_parts, prefix_chunk, row_tiles;
+  size_t pre_slots;
+  size_t own_acc_bytes, own_sum_bytes, pre_acc_bytes, pre_sum_bytes, turns_bytes, bytes;
 };
 
 Plan make_plan(const sale_params_t* p, const sale_cache_t* c, int prefix_len) {
   Plan w = {};
   const int n_rows = p->n_q_heads / p->n_kv_heads * p->seq_len;
-  const long long units = (long long)p->batch * p->n_kv_heads, all_rows = (long long)p->batch * n_rows;
+  const long long all_rows = (long long)p->batch * n_rows;
   auto tiles_for = [](long long rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; };
   auto up = [](long long a, long long b) { return (a + b - 1) / b; };
   auto clamp = [](long long x, long long lo, long long hi) { return (int)(x < lo ? lo : x > hi ? hi : x); };
   w.own_tiles = tiles_for(n_rows);
-  const long long capacity = (long long)c->table_width * c->page_tokens;
-  const long long most = up(capacity, kTurn) < 128 ? up(capacity, kTurn) : 128;
-  const long long wanted = up(1024, units), by_length = up(capacity, 2048);
-  w.own_parts = clamp(wanted > by_length ? wanted : by_length, 1, most);
-  w.own_least = units < 256 ? kTurn : 4 * kTurn;
-  w.direct = w.own_parts == 1 && prefix_len == 0;
+  const long long turns = up((long long)c->table_width * c->page_tokens, kTurn) * p->batch;      // at most
+  w.shares = clamp(up(kShares, p->n_kv_heads), 1, turns);
   if (prefix_len > 0) {
     w.pre_tiles = tiles_for(all_rows);
     w.row_tiles = (int)up(all_rows, 16 * w.pre_tiles);
     const long long groups = (long long)w.row_tiles * p->n_kv_heads;
-    const int parts = clamp(up(1024, groups), 1, up(prefix_len, kTurn) < 128 ? up(prefix_len, kTurn) : 128);
+    const int parts = clamp(up(kShares, groups), 1, up(prefix_len, kTurn) < 128 ? up(prefix_len, kTurn) : 128);
     w.prefix_chunk = (int)(up(up(prefix_len, parts), kTurn) * kTurn);
     w.prefix_parts = (int)up(prefix_len, w.prefix_chunk);
     w.pre_slots = (size_t)groups * w.prefix_parts;
   }
-  w.own_slots = w.direct ? 0 : (size_t)units * w.own_parts;
-  w.own_acc_bytes = w.own_slots * w.own_tiles * 8 * 64 * sizeof(f32x4);
-  w.own_sum_bytes = w.own_slots * w.own_tiles * 16 * sizeof(float2);
-  w.pre_acc_bytes = w.pre_slots * w.pre_tiles * 8 * 64 * sizeof(f32x4);
-  w.pre_sum_bytes = w.pre_slots * w.pre_tiles * 16 * sizeof(float2);
-  w.bytes = w.own_acc_bytes + w.own_sum_bytes + w.pre_acc_bytes + w.pre_sum_bytes;
+  const size_t own_rows = (size_t)p->n_kv_heads * (w.shares + p->batch) * n_rows, pre_rows = w.pre_slots * 16 * w.pre_tiles;
+  auto whole = [](size_t bytes) { return (bytes + 15) & ~(size_t)15; };
+  w.own_acc_bytes = own_rows * kHeadDim * sizeof(float);
+  w.pre_acc_bytes = pre_rows * kHeadDim * sizeof(float);
+  w.own_sum_bytes = whole(own_rows * sizeof(float2));
+  w.pre_sum_bytes = whole(pre_rows * sizeof(float2));
+  w.turns_bytes = (size_t)p->n_kv_heads * p->batch * sizeof(int2);
+  w.bytes = w.own_acc_bytes + w.own_sum_bytes + w.pre_acc_bytes + w.pre_sum_bytes + w.turns_bytes;
   return w;
 }
 
@@ -488,30 +574,25 @@ int validate_decode(const sale_params_t* p, const sale_cache_t* c, int prefix_le
   if (prefix_len < 0) return SALE_ERR_BAD_SHAPE;
   if (prefix_len > 0x3FFFFFFF || p->n_seqs > 0) return SALE_ERR_UNSUPPORTED;
   if ((long long)(p->n_q_heads / p->n_kv_heads) * p->seq_len > 64) return SALE_ERR_UNSUPPORTED;
-  // (workgroups and rows are counted in 32 bits)
+  // (workgroups, rows and turns are counted in 32 bits)
+  if (((long long)c->table_width * c->page_tokens / kTurn + 1) * p->batch > 0x7FFFFFFF) return SALE_ERR_UNSUPPORTED;
   if ((long long)p->batch * p->n_q_heads * p->seq_len > 0x3FFFFFFF || (long long)p->batch * p->n_kv_heads > (0x7FFFFFFF >> 8)) return SALE_ERR_UNSUPPORTED;
   return SALE_OK;
 }
 
 template <bool FP8>
 void launch_decode(const DecodeArgs& a, const Plan& w, hipStream_t st) {
-  const dim3 own((unsigned)((size_t)a.n_seqs * a.n_kvh * a.own_parts)), pre((unsigned)w.pre_slots), threads(64 * kWaves);
+  const dim3 own((unsigned)(a.n_kvh * a.shares)), pre((unsigned)w.pre_slots), threads(64 * kWaves);
   if (w.pre_slots > 0) {
     if (w.pre_tiles == 1) prefix_kernel<FP8, 1><<<pre, threads, 0, st>>>(a);
     else if (w.pre_tiles == 2) prefix_kernel<FP8, 2><<<pre, threads, 0, st>>>(a);
     else prefix_kernel<FP8, 4><<<pre, threads, 0, st>>>(a);
   }
-  if (w.direct) {
-    if (w.own_tiles == 1) own_kernel<FP8, 1, true><<<own, threads, 0, st>>>(a);
-    else if (w.own_tiles == 2) own_kernel<FP8, 2, true><<<own, threads, 0, st>>>(a);
-    else own_kernel<FP8, 4, true><<<own, threads, 0, st>>>(a);
-    return;
-  }
-  if (w.own_tiles == 1) own_kernel<FP8, 1, false><<<own, threads, 0, st>>>(a);
-  else if (w.own_tiles == 2) own_kernel<FP8, 2, false><<<own, threads, 0, st>>>(a);
-  else own_kernel<FP8, 4, false><<<own, threads, 0, st>>>(a);
+  if (w.own_tiles == 1) own_kernel<FP8, 1><<<own, threads, 0, st>>>(a);
+  else if (w.own_tiles == 2) own_kernel<FP8, 2><<<own, threads, 0, st>>>(a);
+  else own_kernel<FP8, 4><<<own, threads, 0, st>>>(a);
   const int n_rows = a.group * a.n_new, tiles = (n_rows + 15) / 16;
-  join_kernel<<<dim3((unsigned)((size_t)a.n_seqs * a.n_kvh * tiles)), dim3(512), 0, st>>>(a, w.own_tiles, w.pre_tiles > 0 ? w.pre_tiles : 1);
+  join_kernel<<<dim3((unsigned)((size_t)a.n_seqs * a.n_kvh * tiles)), dim3(1024), 0, st>>>(a, 16 * (w.pre_tiles > 0 ? w.pre_tiles : 1));
 }
 
 }  // namespace
@@ -532,7 +613,7 @@ extern "C" int sale_decode_attn(const sale_params_t* p, const sale_cache_t* cach
   if (rc != SALE_OK) return rc;
   if (((uintptr_t)q | (uintptr_t)o) & 15) return SALE_ERR_BAD_SHAPE;
   const Plan w = make_plan(p, cache, prefix_len);
-  if (w.bytes > 0 && (!ws || ws_bytes < w.bytes || ((uintptr_t)ws & 15))) return SALE_ERR_WORKSPACE;
+  if (!ws || ws_bytes < w.bytes || ((uintptr_t)ws & 15)) return SALE_ERR_WORKSPACE;
   DecodeArgs a = {};
   a.c = cache_view(p, cache);
   if (cache->dtype != SALE_PAGE_FP8) a.c.k_scale = a.c.v_scale = nullptr;
@@ -547,8 +628,7 @@ extern "C" int sale_decode_attn(const sale_params_t* p, const sale_cache_t* cach
   a.n_new = p->seq_len;
   a.group = p->n_q_heads / p->n_kv_heads;
   a.n_kvh = p->n_kv_heads;
-  a.own_parts = w.own_parts;
-  a.own_least = w.own_least;
+  a.shares = w.shares;
   a.prefix_parts = w.prefix_parts;
   a.prefix_chunk = w.prefix_chunk;
   a.row_tiles = w.row_tiles;
@@ -556,7 +636,8 @@ extern "C" int sale_decode_attn(const sale_params_t* p, const sale_cache_t* cach
   a.own_acc = (f32x4*)at; at += w.own_acc_bytes;
   a.pre_acc = (f32x4*)at; at += w.pre_acc_bytes;
   a.own_sum = (float2*)at; at += w.own_sum_bytes;
-  a.pre_sum = (float2*)at;
+  a.pre_sum = (float2*)at; at += w.pre_sum_bytes;
+  a.turns = (int2*)at;
   if (cache->dtype == SALE_PAGE_FP8) launch_decode<true>(a, w, (hipStream_t)stream);
   else launch_decode<false>(a, w, (hipStream_t)stream);
   return hipGetLastError() == hipSuccess ? SALE_OK : SALE_ERR_HIP;
