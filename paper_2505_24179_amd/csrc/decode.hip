@@ -82,11 +82,17 @@ struct Rows {
   float ref[NT], l[NT];
 };
 
+// An entry of a table at an index that is the same in all lanes.  Through the constant address space, for which the compiler
+// takes a scalar load: a vector load would have to wait for the keys that were requested before it.
+__device__ __forceinline__ int entry_at(const int32_t* table, int i) {
+  return ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)table)[i];
+}
+
 // Pages of the two 16-key tiles of the step at key0 (of its last one that exists where it lies behind it); -1: no page.
 struct TwoPages { int a, b; };
 __device__ __forceinline__ TwoPages pages_of(const CacheView& c, const Keys& ks, int key0) {
   const int last = (ks.n - 1) & ~15;
-  const int a = ks.table[min(key0, last) >> c.page_shift], b = ks.table[min(key0 + 16, last) >> c.page_shift];
+  const int a = entry_at(ks.table, min(key0, last) >> c.page_shift), b = entry_at(ks.table, min(key0 + 16, last) >> c.page_shift);
   return {(unsigned)a < (unsigned)c.n_pages ? a : -1, (unsigned)b < (unsigned)c.n_pages ? b : -1};
 }
 
@@ -155,16 +161,17 @@ __device__ __forceinline__ void one_key(const CacheView& c, Rows<FP8, NT>& rows,
   }
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
+    const std::conditional_t<FP8, u32x2, u32x4> w = ((const std::conditional_t<FP8, u32x2, u32x4>*)v)[r];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       float x;
-      if constexpr (FP8) x = __builtin_amdgcn_cvt_f32_fp8(v[8 * r + e], 0);
-      else x = bf16_bits_to_float(((const uint16_t*)v)[8 * r + e]);
+      if constexpr (FP8) x = __builtin_bit_cast(float, e & 1 ? bf16_pair(w[e >> 2], (e & 2) != 0) & 0xFFFF0000u : bf16_pair(w[e >> 2], (e & 2) != 0) << 16);
+      else x = __builtin_bit_cast(float, e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
 #pragma unroll
       for (int qt = 0; qt < NT; ++qt)
         if (key <= ks.before + rows.token[qt]) rows.acc[qt][e][r] = __builtin_fmaf(pk[qt], x, rows.acc[qt][e][r]);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
@@ -269,6 +276,184 @@ __device__ __forceinline__ void sweep(const CacheView& c, const Keys& ks, int kv
   }
 }
 
+// The same for 64 rows and `steps` steps of which every key is there for every row, key0, key0 + kTurn, ..: a software pipeline.
+// Phase t
+//   S(t + 1) = K(t + 1) Q^T     MFMA
+//   O += V(t - 1)^T P(t - 1)^T  MFMA
+//   P(t) = exp2(S(t) - ref)     VALU, its sums, the turning of V(t - 1) and the largest of the scores S(t + 1)
+//   loads of K(t + 3), V(t + 1) into the registers that were just read
+// has no dependency between its streams; they are laid side by side by hand, an MFMA and its share of the rest at a time, for a
+// wave is alone on its SIMD (64 rows: 128 accumulators, 64 registers of Q, 64 of S, 128 of K and V).
+template <bool FP8>
+__device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int kvh, int key0, int steps, int lane, float scale,
+                                         Rows<FP8, 4>& rows) {
+  constexpr int NT = 4, kQk = 8 * NT, kPv = 8 * NT, kElems = 8 * NT;
+  const int m = lane & 15, g = lane >> 4, mask = (1 << c.page_shift) - 1;
+  const uint32_t row = (uint32_t)(4 * (m & 3) + (m >> 2)) * (uint32_t)c.k.token + 16 * g, col = (uint32_t)g * (uint32_t)c.v.token + (FP8 ? 8 : 16) * m;
+  const uint8_t *k0 = c.k.base + (long long)kvh * c.k.head, *v0 = c.v.base + (long long)kvh * c.v.head;
+  auto key_of = [&](int u) { return key0 + kTurn * min(u, steps - 1); };
+  auto ids_of = [&](int u) -> TwoPages {
+    const int key = key_of(u);
+    return {entry_at(ks.table, key >> c.page_shift), entry_at(ks.table, (key + 16) >> c.page_shift)};
+  };
+  Operands<FP8> x[2];      // [t % 2]
+  auto load_k = [&](Operands<FP8>& to, const uint8_t* (&at)[2], int t, int s) __attribute__((always_inline)) { to.k[t][s] = *(const u32x4*)(at[t] + row + 64 * s); };
+  auto load_v = [&](Operands<FP8>& to, const uint8_t* (&at)[2], int j) __attribute__((always_inline)) {
+    to.v[j] = *(const std::remove_reference_t<decltype(to.v[0])>*)(at[j >> 2] + (long long)(4 * (j & 3)) * c.v.token + col);
+  };
+  auto k_at = [&](int u, TwoPages id, const uint8_t* (&at)[2]) __attribute__((always_inline)) {
+    const int slot = key_of(u) & mask, next = (key_of(u) + 16) & mask;
+    at[0] = k0 + (long long)id.a * c.k.page + (long long)slot * c.k.token;
+    at[1] = k0 + (long long)id.b * c.k.page + (long long)next * c.k.token;
+  };
+  auto v_at = [&](int u, TwoPages id, const uint8_t* (&at)[2]) __attribute__((always_inline)) {
+    const int slot = key_of(u) & mask, next = (key_of(u) + 16) & mask;
+    at[0] = v0 + (long long)id.a * c.v.page + (long long)slot * c.v.token;
+    at[1] = v0 + (long long)id.b * c.v.page + (long long)next * c.v.token;
+  };
+  f32x4 S[2][2][NT];
+  bf16x8 P[2][NT];
+  auto k_operand = [&](const Operands<FP8>& from, int t, int s) __attribute__((always_inline)) -> bf16x8 {
+    if constexpr (FP8) {
+      const u32x4 w = from.k[t][s >> 1];
+      const int h = 2 * (s & 1);
+      return __builtin_bit_cast(bf16x8, u32x4{bf16_pair(w[h], false), bf16_pair(w[h], true), bf16_pair(w[h + 1], false), bf16_pair(w[h + 1], true)});
+    } else {
+      return __builtin_bit_cast(bf16x8, from.k[t][s]);
+    }
+  };
+  // The rows' references follow the scores S[y]; what P holds is still to be added at the old ones: it is scaled like acc.  (ref
+  // is a whole number here, so that is exact.)
+  auto raise = [&](int y, bf16x8 (&pending)[NT]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int qt = 0; qt < NT; ++qt) {
+      float top = S[y][0][qt][0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) top = fmaxf(top, S[y][j >> 2][qt][j & 3]);
+      top = max_over_rows(top) * scale;
+      if (top > rows.ref[qt] - kRoom + kSlack) {
+        const float to = __builtin_ceilf(top) + kRoom, by = __builtin_amdgcn_exp2f(rows.ref[qt] - to);
+        rows.ref[qt] = to;
+        rows.l[qt] *= by;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { rows.acc[qt][e] *= by; pending[qt][e] = (__bf16)((float)pending[qt][e] * by); }
+      }
+    }
+  };
+  const uint8_t* at[2];
+  TwoPages id1 = ids_of(1), id2 = ids_of(2), id3 = ids_of(3);
+  {
+    const TwoPages id0 = ids_of(0);
+    k_at(0, id0, at);
+#pragma unroll
+    for (int n = 0; n < (FP8 ? 4 : 8); ++n) load_k(x[0], at, n / (FP8 ? 2 : 4), n % (FP8 ? 2 : 4));
+    k_at(1, id1, at);
+#pragma unroll
+    for (int n = 0; n < (FP8 ? 4 : 8); ++n) load_k(x[1], at, n / (FP8 ? 2 : 4), n % (FP8 ? 2 : 4));
+    v_at(0, id0, at);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) load_v(x[0], at, j);
+  }
+#pragma unroll
+  for (int n = 0; n < kQk; ++n) {
+    const int t = n / 16, s = n / 4 % 4, qt = n % 4;
+    S[0][t][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand(x[0], t, s), rows.q[qt][s], s == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : S[0][t][qt], 0, 0, 0);
+  }
+  k_at(2, id2, at);
+#pragma unroll
+  for (int n = 0; n < (FP8 ? 4 : 8); ++n) load_k(x[0], at, n / (FP8 ? 2 : 4), n % (FP8 ? 2 : 4));
+#pragma unroll
+  for (int qt = 0; qt < NT; ++qt)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) P[1][qt][e] = (__bf16)0.0f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[1].v[j] = 0;
+  raise(0, P[1]);
+  auto phase = [&](auto xc, int t) __attribute__((always_inline)) {
+    constexpr int cur = decltype(xc)::value, oth = 1 - cur;
+    const uint8_t *k_next[2], *v_next[2];
+    k_at(t + 3, id3, k_next);
+    v_at(t + 1, id1, v_next);
+    id1 = id2; id2 = id3; id3 = ids_of(t + 4);
+    float E[kElems], top[NT];
+    // The VALU stream, four places per score: scale k, exp2 k - 1, sum k - 2, pack the pair that ends with k - 2; then four per
+    // row tile for the maxima of the next scores
+    constexpr int exps = (kElems + 2) * 4, slots = exps + 4 * NT;
+    auto valu = [&](int n) __attribute__((always_inline)) {
+      if (n < exps) {
+        const int k = n / 4, o = n % 4, e = o == 0 ? k : o == 1 ? k - 1 : k - 2;
+        if (e < 0 || e >= kElems) return;
+        const int qt = e / 8, j = e % 8;
+        if (o == 0) E[e] = __builtin_fmaf(S[cur][j >> 2][qt][j & 3], scale, -rows.ref[qt]);
+        else if (o == 1) E[e] = __builtin_amdgcn_exp2f(E[e]);
+        else if (o == 2) rows.l[qt] += E[e];
+        else if (e & 1) { P[cur][qt][j - 1] = (__bf16)E[e - 1]; P[cur][qt][j] = (__bf16)E[e]; }
+      } else {
+        const int qt = (n - exps) % NT, o = (n - exps) / NT;
+        const f32x4 &a = S[oth][0][qt], &b = S[oth][1][qt];
+        auto max3 = [](float p, float q, float r) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(p, q), r); };
+        if (o == 0) top[qt] = max3(a[0], a[1], a[2]);
+        else if (o == 1) top[qt] = max3(top[qt], a[3], b[0]);
+        else if (o == 2) top[qt] = max3(top[qt], b[1], b[2]);
+        else top[qt] = __builtin_elementwise_maximum(top[qt], b[3]);
+      }
+    };
+    bf16x8 k, v[2];
+    static_for<kQk + kPv>([&](auto ic) __attribute__((always_inline)) {
+      constexpr int i = decltype(ic)::value;
+      if constexpr (i < kQk) {
+        constexpr int t2 = i / 16, s = i / 4 % 4, qt = i % 4;
+        if constexpr (qt == 0) k = k_operand(x[oth], t2, s);
+        S[oth][t2][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, rows.q[qt][s], s == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : S[oth][t2][qt], 0, 0, 0);
+        if constexpr (qt == 3 && !FP8) load_k(x[oth], k_next, t2, s);
+        if constexpr (qt == 3 && FP8 && s % 2 == 1) load_k(x[oth], k_next, t2, s / 2);
+        if constexpr (i == kQk - 4) v[0] = turned<FP8>(x[oth], 0);
+      } else {
+        constexpr int e = (i - kQk) / 4, qt = i % 4;
+        rows.acc[qt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[e % 2], P[oth][qt], rows.acc[qt][e], 0, 0, 0);
+        if constexpr (qt == 0 && e < 7) v[(e + 1) % 2] = turned<FP8>(x[oth], e + 1);
+        if constexpr (e >= 6) load_v(x[oth], v_next, 4 * (e - 6) + qt);
+      }
+      constexpr int from = i * slots / (kQk + kPv), to = (i + 1) * slots / (kQk + kPv);
+      static_for<to - from>([&](auto vc) __attribute__((always_inline)) { valu(from + decltype(vc)::value); });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    uint64_t rose = 0;
+#pragma unroll
+    for (int qt = 0; qt < NT; ++qt) rose |= __builtin_amdgcn_ballot_w64(top[qt] * scale > rows.ref[qt] - kRoom + kSlack);
+    if (__builtin_expect_with_probability(rose != 0 && t + 1 < steps, 0, 0.99)) raise(oth, P[cur]);
+  };
+  int t = 0;
+  for (; t + 1 < steps; t += 2) {
+    phase(std::integral_constant<int, 0>{}, t);
+    phase(std::integral_constant<int, 1>{}, t + 1);
+  }
+  auto last = [&](auto xc) __attribute__((always_inline)) {
+    constexpr int cur = decltype(xc)::value;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bf16x8 v = turned<FP8>(x[cur], e);
+#pragma unroll
+      for (int qt = 0; qt < NT; ++qt) rows.acc[qt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[cur][qt], rows.acc[qt][e], 0, 0, 0);
+    }
+  };
+  if (t < steps) {
+    phase(std::integral_constant<int, 0>{}, t);
+    last(std::integral_constant<int, 0>{});
+  } else {
+    last(std::integral_constant<int, 1>{});
+  }
+}
+
+// The sum over the four lanes that are equal modulo 16.
+__device__ __forceinline__ float sum_over_rows(float v) {
+  float w = v;
+  asm volatile("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(v), "+v"(w));
+  w = v = v + w;
+  asm volatile("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(v), "+v"(w));
+  return v + w;
+}
+
 // The results of the four waves, joined.  keep(qt, c, x, l): x = accumulator c of this lane in tile qt, l the sum of its row, for
 // two numbers c per wave; sums(row, ref, l).
 struct JoinLds {
@@ -280,8 +465,7 @@ __device__ __forceinline__ void join_waves(Rows<FP8, NT>& rows, JoinLds& lds, in
   const int n = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int qt = 0; qt < NT; ++qt) {
-    rows.l[qt] += __shfl_xor(rows.l[qt], 16, 64);
-    rows.l[qt] += __shfl_xor(rows.l[qt], 32, 64);
+    rows.l[qt] = sum_over_rows(rows.l[qt]);
     if (g == 0) { lds.ref[wave][16 * qt + n] = rows.ref[qt]; lds.l[wave][16 * qt + n] = rows.l[qt]; }
   }
   __syncthreads();
@@ -326,7 +510,10 @@ __device__ __forceinline__ void load_row(const DecodeArgs& a, int kvh, int s, in
   const RowOf w = row_of(a, r);
   const uint16_t* row = row_at(const_cast<uint16_t*>(a.q), a.sq, s, kvh * a.group + w.head, w.token);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) rows.q[qt][e] = *(const bf16x8*)(row + step_channel<FP8>(e, g));
+  for (int e = 0; e < 4; ++e) {
+    rows.q[qt][e] = *(const bf16x8*)(row + step_channel<FP8>(e, g));
+    if constexpr (NT == 4) asm("" : "+a"(rows.q[qt][e]));      // (what only the matrix unit reads stays out of the ordinary registers)
+  }
   rows.token[qt] = w.token;
   rows.ref[qt] = kNoRef;
   rows.l[qt] = 0.0f;
@@ -354,7 +541,7 @@ template <bool FP8, int NT>
 __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void own_kernel(DecodeArgs a) {
   __shared__ JoinLds lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n = lane & 15, g = lane >> 4, n_rows = a.group * a.n_new;
+  const int n_rows = a.group * a.n_new;
   const int kvh = blockIdx.x % a.n_kvh, j = blockIdx.x / a.n_kvh;
   // lane i counts the turns of sequences i * per ..
   const int per = (a.n_seqs + 63) / 64;
@@ -379,22 +566,27 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void own_kernel(Decod
     const size_t slot = (size_t)kvh * (a.shares + a.n_seqs) + j + s;
     if (from == 0 && tid == 0) a.turns[(size_t)kvh * a.n_seqs + s] = make_int2(base, all);
     Rows<FP8, NT> rows;
+    int from_lane = lane;
+    asm volatile("" : "+v"(from_lane));      // (the addresses of the rows are made here, not kept in registers from piece to piece)
 #pragma unroll
-    for (int qt = 0; qt < NT; ++qt) load_row<FP8, NT>(a, kvh, s, min(16 * qt + n, n_rows - 1), qt, g, rows);
+    for (int qt = 0; qt < NT; ++qt) load_row<FP8, NT>(a, kvh, s, min(16 * qt + (from_lane & 15), n_rows - 1), qt, from_lane >> 4, rows);
     const Keys ks = {a.c.table + (size_t)s * a.c.width, n_keys, min(held - a.n_new + 1, n_keys), held - a.n_new};
     sweep<FP8, NT>(a.c, ks, kvh, lo, hi, wave, lane, a.n_new, scale, rows);
-    join_waves<FP8, NT>(rows, lds, wave, lane,
+    int at_lane = lane;
+    asm volatile("" : "+v"(at_lane));      // (those of the outputs: likewise)
+    const int at_row = at_lane & 15, at_group = at_lane >> 4;
+    join_waves<FP8, NT>(rows, lds, wave, at_lane,
       [&](int qt, int c, f32x4 x, float l) {
-        const int r = 16 * qt + n;
+        const int r = 16 * qt + at_row;
         if (r >= n_rows) return;
         if (whole) {
           const RowOf w = row_of(a, r);
-          uint16_t* out = row_at(a.o, a.so, s, kvh * a.group + w.head, w.token) + 32 * g + c;
+          uint16_t* out = row_at(a.o, a.so, s, kvh * a.group + w.head, w.token) + 32 * at_group + c;
           const float by = l == 0.0f ? 0.0f : v_scale / l;
 #pragma unroll
           for (int e = 0; e < 4; ++e) out[8 * e] = __builtin_bit_cast(uint16_t, (__bf16)(l == 0.0f ? 0.0f : x[e] * by));
         } else {
-          a.own_acc[((slot * 8 + c) * 4 + g) * n_rows + r] = x;
+          a.own_acc[((slot * 8 + c) * 4 + at_group) * n_rows + r] = x;
         }
       },
       [&](int r, float ref, float l) {
@@ -430,7 +622,18 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void prefix_kernel(De
   }
   const Keys ks = {a.prefix_table, a.prefix_len, a.prefix_len, a.prefix_len - 1};
   const float scale = FP8 ? kLog2eByRootD * a.c.k_scale[kvh] : kLog2eByRootD;
-  sweep<FP8, NT>(a.c, ks, kvh, lo, hi, wave, lane, 1, scale, rows);
+  int rest_from = lo;
+  if constexpr (NT == 4) {
+    // whole steps of pages that are there by the pipeline
+    bool missing = false;
+    for (int i = (lo >> a.c.page_shift) + lane; i <= (hi - 1) >> a.c.page_shift; i += 64) missing |= (unsigned)ks.table[i] >= (unsigned)a.c.n_pages;
+    const int first = lo + kStep * wave, whole = max(hi - first, 0) / kStep, steps = (whole + kWaves - 1) / kWaves;
+    if (steps > 0 && __builtin_amdgcn_ballot_w64(missing) == 0) {
+      pipeline<FP8>(a.c, ks, kvh, first, steps, lane, scale, rows);
+      rest_from += steps * kTurn;
+    }
+  }
+  sweep<FP8, NT>(a.c, ks, kvh, rest_from, hi, wave, lane, 1, scale, rows);
   join_waves<FP8, NT>(rows, lds, wave, lane,
     [&](int qt, int c, f32x4 x, float) { a.pre_acc[((slot * 8 + c) * 4 + g) * (16 * NT) + 16 * qt + n] = x; },
     [&](int row, float ref, float l) { a.pre_sum[slot * 16 * NT + row] = make_float2(ref, l); });
