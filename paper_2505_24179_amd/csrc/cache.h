@@ -7,7 +7,8 @@ namespace sale {
 
 struct PageSide {
   uint8_t* base;
-  long long page, head, token;      // bytes
+  long long head;            // bytes, as are
+  uint32_t page, token;
 };
 
 struct CacheView {

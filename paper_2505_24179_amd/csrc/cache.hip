@@ -18,8 +18,13 @@ int validate_cache(const sale_params_t* p, const sale_cache_t* c, bool tables) {
     if (st[0] == 0 && st[1] == 0 && st[2] == 0) continue;
     for (int e = 0; e < 3; ++e)
       if (st[e] < 0 || st[e] % unit) return SALE_ERR_BAD_SHAPE;
-    if (st[2] < kHeadDim || st[2] > (1 << 24)) return SALE_ERR_BAD_SHAPE;
+    if (st[2] < kHeadDim) return SALE_ERR_BAD_SHAPE;
     if ((p->n_kv_heads > 1 && st[1] == 0) || (c->n_pages > 1 && st[0] == 0)) return SALE_ERR_BAD_SHAPE;
+  }
+  // (strides of pages and tokens are 32-bit numbers of bytes in the kernels, and so is a token's place in its page)
+  for (const int64_t* st : triples) {
+    const int64_t page = st[0] | st[1] | st[2] ? st[0] : (int64_t)p->n_kv_heads * c->page_tokens * kHeadDim;
+    if (page > 0xFFFFFFFFLL / (16 / unit) || st[2] > (1 << 22)) return SALE_ERR_UNSUPPORTED;
   }
   if (c->dtype == SALE_PAGE_FP8 && tables && (!c->k_scale || !c->v_scale)) return SALE_ERR_NULL_ARG;
   if (!tables) return SALE_OK;
@@ -34,9 +39,9 @@ CacheView cache_view(const sale_params_t* p, const sale_cache_t* c) {
   auto side = [&](void* base, const int64_t* st) -> PageSide {
     if (st[0] == 0 && st[1] == 0 && st[2] == 0) {
       const long long token = kHeadDim * size, head = token * c->page_tokens;
-      return {(uint8_t*)base, head * p->n_kv_heads, head, token};
+      return {(uint8_t*)base, head, (uint32_t)(head * p->n_kv_heads), (uint32_t)token};
     }
-    return {(uint8_t*)base, st[0] * size, st[1] * size, st[2] * size};
+    return {(uint8_t*)base, st[1] * size, (uint32_t)(st[0] * size), (uint32_t)(st[2] * size)};
   };
   return {side(c->k, c->k_stride), side(c->v, c->v_stride), c->k_scale, c->v_scale, c->table, c->lens, c->n_pages,
           __builtin_ctz((unsigned)c->page_tokens), c->table_width};
@@ -59,9 +64,19 @@ struct AppendJob {
   int token[kAppendChunk + 1], at[kAppendChunk + 1];      // first token and first workgroup of a sequence
 };
 
-// e4m3 of two values: nearest, ties to even; at most 448 in size; NaN stays.
-__device__ __forceinline__ float limit448(float x) { return x != x ? x : fminf(fmaxf(x, -448.0f), 448.0f); }
-__device__ __forceinline__ u32x2 to_fp8(u32x4 w, float scale) {
+// e4m3(x / scale), nearest, ties to even; at most 448 in size; NaN stays.  The quotient is the correctly rounded one: with
+// inv = 1 / scale correctly rounded, q = x inv is next to it and one step of Newton's with the exact remainder gives it (Markstein,
+// 1990), in 3 instructions where the compiler's division takes 10.  Quotients of 1000 and more are only limited; a scale so far
+// out that remainders could leave the range of a float takes the division.
+struct Divisor { float scale, inv; bool far; };
+__device__ __forceinline__ Divisor divisor(float scale) { return {scale, 1.0f / scale, !(scale >= 0x1p-60f && scale <= 0x1p60f)}; }
+__device__ __forceinline__ float quotient448(float x, const Divisor& d) {
+  float q = x * d.inv;
+  if (d.far) q = x / d.scale;
+  else if (__builtin_fabsf(q) < 1000.0f) q = __builtin_fmaf(__builtin_fmaf(-q, d.scale, x), d.inv, q);
+  return q != q ? q : __builtin_amdgcn_fmed3f(q, -448.0f, 448.0f);
+}
+__device__ __forceinline__ u32x2 to_fp8(u32x4 w, const Divisor& d) {
   u32x2 out;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -70,7 +85,7 @@ __device__ __forceinline__ u32x2 to_fp8(u32x4 w, float scale) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const uint32_t word = w[2 * h + (e >> 1)];
-      x[e] = limit448(__builtin_bit_cast(float, e & 1 ? word & 0xFFFF0000u : word << 16) / scale);
+      x[e] = quotient448(__builtin_bit_cast(float, e & 1 ? word & 0xFFFF0000u : word << 16), d);
     }
     r = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], r, false);
     r = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], r, true);
@@ -102,21 +117,34 @@ __global__ __launch_bounds__(256) void append_kernel(AppendJob a) {
   const int start = max(a.c.lens[s], 0) - n_new;      // position of the sequence's first new token
   const int32_t* table = a.c.table + (size_t)s * a.c.width;
   const int batch = a.each > 0 ? s : 0;
-  for (int id = threadIdx.x; id < 2 * rows * 16; id += 256) {
-    const bool is_v = id >= rows * 16;
-    const int row = (is_v ? id - rows * 16 : id) >> 4, chunk = id & 15;
-    const int h = a.heads_first ? row % a.n_kvh : row / count, i = a.heads_first ? row / a.n_kvh : row % count;
-    const int pos = start + t0 + i;
-    if (pos < 0 || pos >> a.c.page_shift >= a.c.width) continue;
-    const int page = table[pos >> a.c.page_shift], slot = pos & ((1 << a.c.page_shift) - 1);
-    if ((unsigned)page >= (unsigned)a.c.n_pages) continue;
-    const Strided& ss = is_v ? a.sv : a.sk;
-    const size_t from = 2 * ((size_t)batch * ss.sb + (size_t)h * ss.sh + (size_t)(first + t0 + i) * ss.st) + 16 * chunk;
-    const u32x4 w = *(const u32x4*)((is_v ? a.v : a.k) + from);
-    const PageSide& side = is_v ? a.c.v : a.c.k;
-    uint8_t* to = side.base + (long long)page * side.page + (long long)h * side.head + (long long)slot * side.token;
-    if constexpr (FP8) *(u32x2*)(to + 8 * chunk) = to_fp8(w, (is_v ? a.c.v_scale : a.c.k_scale)[h]);
-    else *(u32x4*)(to + 16 * chunk) = w;
+  // (four turns at a time: their page numbers and tokens are in flight together)
+  for (int id0 = threadIdx.x; id0 < 2 * rows * 16; id0 += 4 * 256) {
+    u32x4 w[4];
+    int page[4], pos[4], head[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int id = min(id0 + 256 * u, 2 * rows * 16 - 1);
+      const bool is_v = id >= rows * 16;
+      const int row = (is_v ? id - rows * 16 : id) >> 4;
+      const int h = a.heads_first ? row % a.n_kvh : row / count, i = a.heads_first ? row / a.n_kvh : row % count;
+      head[u] = h;
+      pos[u] = start + t0 + i;
+      const bool place = pos[u] >= 0 && pos[u] >> a.c.page_shift < a.c.width && id0 + 256 * u < 2 * rows * 16;
+      page[u] = place ? table[pos[u] >> a.c.page_shift] : -1;
+      const Strided& ss = is_v ? a.sv : a.sk;
+      w[u] = *(const u32x4*)((is_v ? a.v : a.k) + 2 * ((size_t)batch * ss.sb + (size_t)h * ss.sh + (size_t)(first + t0 + i) * ss.st) + 16 * (id & 15));
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if ((unsigned)page[u] >= (unsigned)a.c.n_pages) continue;
+      const bool is_v = id0 + 256 * u >= rows * 16;
+      const PageSide& side = is_v ? a.c.v : a.c.k;
+      uint8_t* to = side.base + (uint64_t)(uint32_t)page[u] * side.page + (long long)head[u] * side.head +
+                    (uint64_t)(uint32_t)(pos[u] & ((1 << a.c.page_shift) - 1)) * side.token;
+      const int chunk = id0 & 15;
+      if constexpr (FP8) *(u32x2*)(to + 8 * chunk) = to_fp8(w[u], divisor((is_v ? a.c.v_scale : a.c.k_scale)[head[u]]));
+      else *(u32x4*)(to + 16 * chunk) = w[u];
+    }
   }
 }
 

@@ -96,22 +96,41 @@ __device__ __forceinline__ TwoPages pages_of(const CacheView& c, const Keys& ks,
   return {(unsigned)a < (unsigned)c.n_pages ? a : -1, (unsigned)b < (unsigned)c.n_pages ? b : -1};
 }
 
+// Token slots slot .. slot + 15 of a page of one KV head, as a buffer: a load's address is then a scalar base, a lane's offset that
+// stays and a scalar or constant one, without a vector instruction.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t slots_of(const PageSide& side, const uint8_t* head, int page, int slot) {
+  return operand_buffer(head + (uint64_t)(uint32_t)page * side.page + (uint32_t)slot * side.token, 0x7FFFFFF0);
+}
+// Offsets of a lane: of the key row and channels that it loads of K, and of V.
+struct LaneOffsets { int k, v; };
 template <bool FP8>
-__device__ __forceinline__ void load_step(const CacheView& c, const Keys& ks, int kvh, int key0, TwoPages pg, int m, int g, Operands<FP8>& x) {
+__device__ __forceinline__ LaneOffsets lane_offsets(const CacheView& c, int lane) {
+  const int m = lane & 15, g = lane >> 4;
+  return {(int)((4 * (m & 3) + (m >> 2)) * c.k.token) + 16 * g, (int)(g * c.v.token) + (FP8 ? 8 : 16) * m};
+}
+template <bool FP8>
+__device__ __forceinline__ void load_k(Operands<FP8>& x, int t, int s, __amdgpu_buffer_rsrc_t from, int lane_offset) {
+  x.k[t][s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, lane_offset + 64 * s, 0, 0));
+}
+template <bool FP8>
+__device__ __forceinline__ void load_v(Operands<FP8>& x, int j, __amdgpu_buffer_rsrc_t from, int lane_offset, uint32_t token) {
+  if constexpr (FP8) x.v[j] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(from, lane_offset, 4 * (j & 3) * token, 0));
+  else x.v[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, lane_offset, 4 * (j & 3) * token, 0));
+}
+
+template <bool FP8>
+__device__ __forceinline__ void load_step(const CacheView& c, const Keys& ks, int kvh, int key0, TwoPages pg, LaneOffsets at, Operands<FP8>& x) {
   const int last = (ks.n - 1) & ~15, mask = (1 << c.page_shift) - 1;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const int page = t == 0 ? pg.a : pg.b;
+    const int page = max(t == 0 ? pg.a : pg.b, 0);      // (without a page: any one, whose keys are not used)
     const int slot = min(key0 + 16 * t, last) & mask;
-    const long long at = page < 0 ? 0 : page;      // (without a page: any one, whose keys are not used)
-    const uint8_t* kb = c.k.base + at * c.k.page + (long long)kvh * c.k.head + (long long)slot * c.k.token;
-    const uint32_t row = (uint32_t)(4 * (m & 3) + (m >> 2)) * (uint32_t)c.k.token + 16 * g;
+    const __amdgpu_buffer_rsrc_t k = slots_of(c.k, c.k.base + (long long)kvh * c.k.head, page, slot);
+    const __amdgpu_buffer_rsrc_t v = slots_of(c.v, c.v.base + (long long)kvh * c.v.head, page, slot);
 #pragma unroll
-    for (int s = 0; s < (FP8 ? 2 : 4); ++s) x.k[t][s] = *(const u32x4*)(kb + row + 64 * s);
-    const uint8_t* vb = c.v.base + at * c.v.page + (long long)kvh * c.v.head + (long long)slot * c.v.token;
-    const uint32_t col = (uint32_t)g * (uint32_t)c.v.token + (FP8 ? 8 : 16) * m;
+    for (int s = 0; s < (FP8 ? 2 : 4); ++s) load_k<FP8>(x, t, s, k, at.k);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) x.v[4 * t + r] = *(const std::remove_reference_t<decltype(x.v[0])>*)(vb + (long long)(4 * r) * c.v.token + col);
+    for (int r = 0; r < 4; ++r) load_v<FP8>(x, 4 * t + r, v, at.v, c.v.token);
   }
 }
 
@@ -263,20 +282,21 @@ __device__ __forceinline__ void step(const CacheView& c, Operands<FP8>& x, Rows<
   }
 }
 
-// Keys lo .. hi - 1 for the rows, by the waves of the workgroup in turn.
+// Keys from .. hi - 1 for the rows, 32 of every kTurn.
 template <bool FP8, int NT>
-__device__ __forceinline__ void sweep(const CacheView& c, const Keys& ks, int kvh, int lo, int hi, int wave, int lane, int n_new, float scale,
+__device__ __forceinline__ void sweep(const CacheView& c, const Keys& ks, int kvh, int from, int hi, int lane, int n_new, float scale,
                                       Rows<FP8, NT>& rows) {
-  const int m = lane & 15, g = lane >> 4;
-  for (int key0 = lo + kStep * wave; key0 < hi; key0 += kTurn) {
+  const LaneOffsets at = lane_offsets<FP8>(c, lane);
+  for (int key0 = from; key0 < hi; key0 += kTurn) {
     const TwoPages pg = pages_of(c, ks, key0);
     Operands<FP8> x;
-    load_step<FP8>(c, ks, kvh, key0, pg, m, g, x);
-    step<FP8, NT>(c, x, rows, scale, ks, kvh, key0, pg, key0 + kStep > ks.all || (pg.a | pg.b) < 0, g, n_new);
+    load_step<FP8>(c, ks, kvh, key0, pg, at, x);
+    step<FP8, NT>(c, x, rows, scale, ks, kvh, key0, pg, key0 + kStep > ks.all || (pg.a | pg.b) < 0, lane >> 4, n_new);
   }
 }
 
-// The same for 64 rows and `steps` steps of which every key is there for every row, key0, key0 + kTurn, ..: a software pipeline.
+// The same for 64 rows and `steps` steps, an even number, of which every key is there for every row, key0, key0 + kTurn, ..: a
+// software pipeline.
 // Phase t
 //   S(t + 1) = K(t + 1) Q^T     MFMA
 //   O += V(t - 1)^T P(t - 1)^T  MFMA
@@ -284,32 +304,47 @@ __device__ __forceinline__ void sweep(const CacheView& c, const Keys& ks, int kv
 //   loads of K(t + 3), V(t + 1) into the registers that were just read
 // has no dependency between its streams; they are laid side by side by hand, an MFMA and its share of the rest at a time, for a
 // wave is alone on its SIMD (64 rows: 128 accumulators, 64 registers of Q, 64 of S, 128 of K and V).
-template <bool FP8>
+template <bool FP8, bool ONE>
 __device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int kvh, int key0, int steps, int lane, float scale,
                                          Rows<FP8, 4>& rows) {
-  constexpr int NT = 4, kQk = 8 * NT, kPv = 8 * NT, kElems = 8 * NT;
-  const int m = lane & 15, g = lane >> 4, mask = (1 << c.page_shift) - 1;
-  const uint32_t row = (uint32_t)(4 * (m & 3) + (m >> 2)) * (uint32_t)c.k.token + 16 * g, col = (uint32_t)g * (uint32_t)c.v.token + (FP8 ? 8 : 16) * m;
-  const uint8_t *k0 = c.k.base + (long long)kvh * c.k.head, *v0 = c.v.base + (long long)kvh * c.v.head;
+  constexpr int NT = 4, kQk = 8 * NT, kPv = 8 * NT, kElems = 8 * NT, kLoads = FP8 ? 2 : 4;
+  const int mask = (1 << c.page_shift) - 1;
+  const LaneOffsets lane_at = lane_offsets<FP8>(c, lane);
+  const uint8_t *k_head = c.k.base + (long long)kvh * c.k.head, *v_head = c.v.base + (long long)kvh * c.v.head;
+  // Where the 16-key tiles of step u are: their pages (one where a step lies in a page) and first slots
   auto key_of = [&](int u) { return key0 + kTurn * min(u, steps - 1); };
   auto ids_of = [&](int u) -> TwoPages {
-    const int key = key_of(u);
-    return {entry_at(ks.table, key >> c.page_shift), entry_at(ks.table, (key + 16) >> c.page_shift)};
+    const int key = key_of(u), a = entry_at(ks.table, key >> c.page_shift);
+    return {a, ONE ? a : entry_at(ks.table, (key + 16) >> c.page_shift)};
+  };
+  struct Tiles { __amdgpu_buffer_rsrc_t a, b; };
+  auto tiles_of = [&](const PageSide& side, const uint8_t* head, int u, TwoPages id) __attribute__((always_inline)) -> Tiles {
+    const int slot = key_of(u) & mask;
+    if constexpr (ONE) {
+      const uint8_t* at = head + (uint64_t)(uint32_t)id.a * side.page + (uint32_t)slot * side.token;
+      return {operand_buffer(at, 0x7FFFFFF0), operand_buffer(at + 16 * side.token, 0x7FFFFFF0)};
+    } else {
+      return {slots_of(side, head, id.a, slot), slots_of(side, head, id.b, (slot + 16) & mask)};
+    }
   };
   Operands<FP8> x[2];      // [t % 2]
-  auto load_k = [&](Operands<FP8>& to, const uint8_t* (&at)[2], int t, int s) __attribute__((always_inline)) { to.k[t][s] = *(const u32x4*)(at[t] + row + 64 * s); };
-  auto load_v = [&](Operands<FP8>& to, const uint8_t* (&at)[2], int j) __attribute__((always_inline)) {
-    to.v[j] = *(const std::remove_reference_t<decltype(to.v[0])>*)(at[j >> 2] + (long long)(4 * (j & 3)) * c.v.token + col);
+  auto get_k = [&](Operands<FP8>& to, const Tiles& from, int t, int s) __attribute__((always_inline)) { load_k<FP8>(to, t, s, t == 0 ? from.a : from.b, lane_at.k); };
+  auto get_v = [&](Operands<FP8>& to, const Tiles& from, int j) __attribute__((always_inline)) { load_v<FP8>(to, j, j < 4 ? from.a : from.b, lane_at.v, c.v.token); };
+  // O += V P with the accumulators in AGPRs, where the compiler would move them back and forth: S, P and V take most of the 256
+  // ordinary registers.  The compiler does not see a matrix instruction here, so its waits are this code's to keep: 2 states from
+  // what writes v, p or acc to the product (in a phase 3 other products are between, elsewhere s_nop 1), and from the product to
+  // what else reads acc, settle.
+  auto pv = [&](auto close, int qt, int e, const bf16x8& v, const bf16x8& p) __attribute__((always_inline)) {
+    f32x4& acc = rows.acc[qt][e];
+    if constexpr (decltype(close)::value) asm("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(v), "v"(p));
+    else asm("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(v), "v"(p));
   };
-  auto k_at = [&](int u, TwoPages id, const uint8_t* (&at)[2]) __attribute__((always_inline)) {
-    const int slot = key_of(u) & mask, next = (key_of(u) + 16) & mask;
-    at[0] = k0 + (long long)id.a * c.k.page + (long long)slot * c.k.token;
-    at[1] = k0 + (long long)id.b * c.k.page + (long long)next * c.k.token;
-  };
-  auto v_at = [&](int u, TwoPages id, const uint8_t* (&at)[2]) __attribute__((always_inline)) {
-    const int slot = key_of(u) & mask, next = (key_of(u) + 16) & mask;
-    at[0] = v0 + (long long)id.a * c.v.page + (long long)slot * c.v.token;
-    at[1] = v0 + (long long)id.b * c.v.page + (long long)next * c.v.token;
+  auto settle = [&]() __attribute__((always_inline)) {
+    asm volatile("s_nop 15\n\ts_nop 15");
+#pragma unroll
+    for (int qt = 0; qt < NT; ++qt)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) asm volatile("" : "+a"(rows.acc[qt][e]));
   };
   f32x4 S[2][2][NT];
   bf16x8 P[2][NT];
@@ -325,6 +360,7 @@ __device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int
   // The rows' references follow the scores S[y]; what P holds is still to be added at the old ones: it is scaled like acc.  (ref
   // is a whole number here, so that is exact.)
   auto raise = [&](int y, bf16x8 (&pending)[NT]) __attribute__((always_inline)) {
+    settle();
 #pragma unroll
     for (int qt = 0; qt < NT; ++qt) {
       float top = S[y][0][qt][0];
@@ -340,28 +376,26 @@ __device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int
       }
     }
   };
-  const uint8_t* at[2];
   TwoPages id1 = ids_of(1), id2 = ids_of(2), id3 = ids_of(3);
+  auto get_all_k = [&](Operands<FP8>& to, int u, TwoPages id) __attribute__((always_inline)) {
+    const Tiles from = tiles_of(c.k, k_head, u, id);
+#pragma unroll
+    for (int n = 0; n < 2 * kLoads; ++n) get_k(to, from, n / kLoads, n % kLoads);
+  };
   {
     const TwoPages id0 = ids_of(0);
-    k_at(0, id0, at);
+    get_all_k(x[0], 0, id0);
+    get_all_k(x[1], 1, id1);
+    const Tiles from = tiles_of(c.v, v_head, 0, id0);
 #pragma unroll
-    for (int n = 0; n < (FP8 ? 4 : 8); ++n) load_k(x[0], at, n / (FP8 ? 2 : 4), n % (FP8 ? 2 : 4));
-    k_at(1, id1, at);
-#pragma unroll
-    for (int n = 0; n < (FP8 ? 4 : 8); ++n) load_k(x[1], at, n / (FP8 ? 2 : 4), n % (FP8 ? 2 : 4));
-    v_at(0, id0, at);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) load_v(x[0], at, j);
+    for (int j = 0; j < 8; ++j) get_v(x[0], from, j);
   }
 #pragma unroll
   for (int n = 0; n < kQk; ++n) {
     const int t = n / 16, s = n / 4 % 4, qt = n % 4;
     S[0][t][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand(x[0], t, s), rows.q[qt][s], s == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : S[0][t][qt], 0, 0, 0);
   }
-  k_at(2, id2, at);
-#pragma unroll
-  for (int n = 0; n < (FP8 ? 4 : 8); ++n) load_k(x[0], at, n / (FP8 ? 2 : 4), n % (FP8 ? 2 : 4));
+  get_all_k(x[0], 2, id2);
 #pragma unroll
   for (int qt = 0; qt < NT; ++qt)
 #pragma unroll
@@ -371,9 +405,7 @@ __device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int
   raise(0, P[1]);
   auto phase = [&](auto xc, int t) __attribute__((always_inline)) {
     constexpr int cur = decltype(xc)::value, oth = 1 - cur;
-    const uint8_t *k_next[2], *v_next[2];
-    k_at(t + 3, id3, k_next);
-    v_at(t + 1, id1, v_next);
+    const Tiles k_next = tiles_of(c.k, k_head, t + 3, id3), v_next = tiles_of(c.v, v_head, t + 1, id1);
     id1 = id2; id2 = id3; id3 = ids_of(t + 4);
     float E[kElems], top[NT];
     // The VALU stream, four places per score: scale k, exp2 k - 1, sum k - 2, pack the pair that ends with k - 2; then four per
@@ -405,14 +437,14 @@ __device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int
         constexpr int t2 = i / 16, s = i / 4 % 4, qt = i % 4;
         if constexpr (qt == 0) k = k_operand(x[oth], t2, s);
         S[oth][t2][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, rows.q[qt][s], s == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : S[oth][t2][qt], 0, 0, 0);
-        if constexpr (qt == 3 && !FP8) load_k(x[oth], k_next, t2, s);
-        if constexpr (qt == 3 && FP8 && s % 2 == 1) load_k(x[oth], k_next, t2, s / 2);
+        if constexpr (qt == 3 && !FP8) get_k(x[oth], k_next, t2, s);
+        if constexpr (qt == 3 && FP8 && s % 2 == 1) get_k(x[oth], k_next, t2, s / 2);
         if constexpr (i == kQk - 4) v[0] = turned<FP8>(x[oth], 0);
       } else {
         constexpr int e = (i - kQk) / 4, qt = i % 4;
-        rows.acc[qt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[e % 2], P[oth][qt], rows.acc[qt][e], 0, 0, 0);
+        pv(std::false_type{}, qt, e, v[e % 2], P[oth][qt]);
         if constexpr (qt == 0 && e < 7) v[(e + 1) % 2] = turned<FP8>(x[oth], e + 1);
-        if constexpr (e >= 6) load_v(x[oth], v_next, 4 * (e - 6) + qt);
+        if constexpr (e >= 6) get_v(x[oth], v_next, 4 * (e - 6) + qt);
       }
       constexpr int from = i * slots / (kQk + kPv), to = (i + 1) * slots / (kQk + kPv);
       static_for<to - from>([&](auto vc) __attribute__((always_inline)) { valu(from + decltype(vc)::value); });
@@ -423,26 +455,18 @@ __device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int
     for (int qt = 0; qt < NT; ++qt) rose |= __builtin_amdgcn_ballot_w64(top[qt] * scale > rows.ref[qt] - kRoom + kSlack);
     if (__builtin_expect_with_probability(rose != 0 && t + 1 < steps, 0, 0.99)) raise(oth, P[cur]);
   };
-  int t = 0;
-  for (; t + 1 < steps; t += 2) {
+  for (int t = 0; t < steps; t += 2) {
     phase(std::integral_constant<int, 0>{}, t);
     phase(std::integral_constant<int, 1>{}, t + 1);
   }
-  auto last = [&](auto xc) __attribute__((always_inline)) {
-    constexpr int cur = decltype(xc)::value;
+  settle();
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const bf16x8 v = turned<FP8>(x[cur], e);
+  for (int e = 0; e < 8; ++e) {
+    const bf16x8 v = turned<FP8>(x[1], e);
 #pragma unroll
-      for (int qt = 0; qt < NT; ++qt) rows.acc[qt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[cur][qt], rows.acc[qt][e], 0, 0, 0);
-    }
-  };
-  if (t < steps) {
-    phase(std::integral_constant<int, 0>{}, t);
-    last(std::integral_constant<int, 0>{});
-  } else {
-    last(std::integral_constant<int, 1>{});
+    for (int qt = 0; qt < NT; ++qt) pv(std::true_type{}, qt, e, v, P[1][qt]);
   }
+  settle();
 }
 
 // The sum over the four lanes that are equal modulo 16.
@@ -499,16 +523,17 @@ __device__ __forceinline__ float lse_of(float ref, float l) { return l == 0.0f ?
 
 // Row r of a sequence: its new token and the query head inside its group.
 struct RowOf { int token, head; };
-__device__ __forceinline__ RowOf row_of(const DecodeArgs& a, int r) { const int t = r / a.group; return {t, r - t * a.group}; }
+__device__ __forceinline__ RowOf row_of(int group, int r) { const int t = r / group; return {t, r - t * group}; }
 
 __device__ __forceinline__ uint16_t* row_at(uint16_t* x, const Strided& l, int s, int head, int token) {
   return x + (size_t)s * (size_t)l.sb + (size_t)head * (size_t)l.sh + (size_t)token * (size_t)l.st;
 }
 
 template <bool FP8, int NT>
-__device__ __forceinline__ void load_row(const DecodeArgs& a, int kvh, int s, int r, int qt, int g, Rows<FP8, NT>& rows) {
-  const RowOf w = row_of(a, r);
-  const uint16_t* row = row_at(const_cast<uint16_t*>(a.q), a.sq, s, kvh * a.group + w.head, w.token);
+__device__ __forceinline__ void load_row(const uint16_t* q, const Strided& sq, int group, int kvh, int s, int r, int qt, int g,
+                                         Rows<FP8, NT>& rows) {
+  const RowOf w = row_of(group, r);
+  const uint16_t* row = row_at(const_cast<uint16_t*>(q), sq, s, kvh * group + w.head, w.token);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     rows.q[qt][e] = *(const bf16x8*)(row + step_channel<FP8>(e, g));
@@ -523,8 +548,7 @@ __device__ __forceinline__ void load_row(const DecodeArgs& a, int kvh, int s, in
 
 // Sharing out the own keys.  A sequence has as many turns as workgroups need to read its keys, kTurn at a time; the turns of
 // all sequences, one after the other, are dealt to the workgroups of a KV head in equal shares.
-__device__ __forceinline__ int keys_of(const CacheView& c, int s) { return min(max(c.lens[s], 0), c.width << c.page_shift); }
-__device__ __forceinline__ int turns_of(const CacheView& c, int s) { return (keys_of(c, s) + kTurn - 1) / kTurn; }
+__device__ __forceinline__ int turns_of(const CacheView& c, int len) { return (min(max(len, 0), c.width << c.page_shift) + kTurn - 1) / kTurn; }
 struct Share { long long first, count; };
 __device__ __forceinline__ Share share_of(long long turns, int shares, int j) {
   const long long each = turns / shares, more = turns - each * shares;      // (the first `more` shares have one turn more)
@@ -536,17 +560,65 @@ __device__ __forceinline__ int share_with(long long turns, int shares, long long
 }
 
 // A workgroup: one share of the turns of a KV head, piece by piece (a piece: neighbouring turns of one sequence).  The only piece
-// of a sequence, without a prefix, is its result.
-template <bool FP8, int NT>
+// of a sequence, without a prefix, is its result.  WHOLE: workgroup j has all of sequence j, and there is nothing to join.
+template <bool FP8, int NT, bool WHOLE>
 __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void own_kernel(DecodeArgs a) {
   __shared__ JoinLds lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_rows = a.group * a.n_new;
   const int kvh = blockIdx.x % a.n_kvh, j = blockIdx.x / a.n_kvh;
+  const float scale = FP8 ? kLog2eByRootD * a.c.k_scale[kvh] : kLog2eByRootD, v_scale = FP8 ? a.c.v_scale[kvh] : 1.0f;
+  // Turns from .. from + count - 1 of sequence s; whole: they are all it has, and the result.
+  auto piece = [&](int s, int from, int count, bool whole) __attribute__((always_inline)) {
+    const int held = max(entry_at(a.c.lens, s), 0), n_keys = min(held, a.c.width << a.c.page_shift);
+    const int lo = from * kTurn, hi = min((from + count) * kTurn, n_keys);
+    const size_t slot = (size_t)kvh * (a.shares + a.n_seqs) + j + s;
+    Rows<FP8, NT> rows;
+    // (The addresses of the rows, and of the outputs below, are made here, from arguments that are read here: nothing of them stays
+    // in registers from piece to piece or during the sweep.)
+    int from_lane = lane;
+    auto args = (const __attribute__((address_space(4))) DecodeArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+v"(from_lane), "+s"(args));
+    const Strided sq = {args->sq.sb, args->sq.sh, args->sq.st, args->sq.heads};
+#pragma unroll
+    for (int qt = 0; qt < NT; ++qt)
+      load_row<FP8, NT>(args->q, sq, a.group, kvh, s, min(16 * qt + (from_lane & 15), n_rows - 1), qt, from_lane >> 4, rows);
+    const Keys ks = {a.c.table + (size_t)s * a.c.width, n_keys, min(held - a.n_new + 1, n_keys), held - a.n_new};
+    sweep<FP8, NT>(a.c, ks, kvh, lo + kStep * wave, hi, from_lane, a.n_new, scale, rows);
+    int at_lane = from_lane;
+    auto late = (const __attribute__((address_space(4))) DecodeArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+v"(at_lane), "+s"(late));
+    const int at_row = at_lane & 15, at_group = at_lane >> 4;
+    const Strided so = {late->so.sb, late->so.sh, late->so.st, late->so.heads};
+    join_waves<FP8, NT>(rows, lds, wave, at_lane,
+      [&](int qt, int c, f32x4 x, float l) {
+        const int r = 16 * qt + at_row;
+        if (r >= n_rows) return;
+        if (whole) {
+          const RowOf w = row_of(a.group, r);
+          uint16_t* out = row_at(late->o, so, s, kvh * a.group + w.head, w.token) + 32 * at_group + c;
+          const float by = l == 0.0f ? 0.0f : v_scale / l;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) out[8 * e] = __builtin_bit_cast(uint16_t, (__bf16)(l == 0.0f ? 0.0f : x[e] * by));
+        } else {
+          late->own_acc[((slot * 8 + c) * 4 + at_group) * n_rows + r] = x;
+        }
+      },
+      [&](int r, float ref, float l) {
+        if (r >= n_rows) return;
+        if (whole) {
+          const RowOf w = row_of(a.group, r);
+          if (late->lse) late->lse[((size_t)s * so.heads + kvh * a.group + w.head) * a.n_new + w.token] = lse_of(ref, l);
+        } else {
+          late->own_sum[slot * n_rows + r] = make_float2(ref, l);
+        }
+      });
+  };
+  if (WHOLE) { piece(j, 0, turns_of(a.c, entry_at(a.c.lens, j)), true); return; }
   // lane i counts the turns of sequences i * per ..
   const int per = (a.n_seqs + 63) / 64;
   int mine = 0;
-  for (int s = lane * per; s < min((lane + 1) * per, a.n_seqs); ++s) mine += turns_of(a.c, s);
+  for (int s = lane * per; s < min((lane + 1) * per, a.n_seqs); ++s) mine += turns_of(a.c, a.c.lens[s]);
   int upto = mine;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) { const int x = __shfl_up(upto, d, 64); if (lane >= d) upto += x; }
@@ -555,51 +627,15 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void own_kernel(Decod
   if (share.count == 0) return;
   const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > share.first));
   int s = at * per, base = __builtin_amdgcn_readlane(upto - mine, at), left = (int)share.count;      // base: first turn of sequence s
-  const float scale = FP8 ? kLog2eByRootD * a.c.k_scale[kvh] : kLog2eByRootD, v_scale = FP8 ? a.c.v_scale[kvh] : 1.0f;
   int turn = (int)share.first;
   for (; left > 0; ++s) {
-    const int held = max(a.c.lens[s], 0), n_keys = keys_of(a.c, s), turns = (n_keys + kTurn - 1) / kTurn;
-    if (turn >= base + turns) { base += turns; continue; }
-    const int from = turn - base, count = min(turns - from, left);
-    const int lo = from * kTurn, hi = min((from + count) * kTurn, n_keys);
-    const bool whole = count == turns && a.prefix_len == 0;
-    const size_t slot = (size_t)kvh * (a.shares + a.n_seqs) + j + s;
-    if (from == 0 && tid == 0) a.turns[(size_t)kvh * a.n_seqs + s] = make_int2(base, all);
-    Rows<FP8, NT> rows;
-    int from_lane = lane;
-    asm volatile("" : "+v"(from_lane));      // (the addresses of the rows are made here, not kept in registers from piece to piece)
-#pragma unroll
-    for (int qt = 0; qt < NT; ++qt) load_row<FP8, NT>(a, kvh, s, min(16 * qt + (from_lane & 15), n_rows - 1), qt, from_lane >> 4, rows);
-    const Keys ks = {a.c.table + (size_t)s * a.c.width, n_keys, min(held - a.n_new + 1, n_keys), held - a.n_new};
-    sweep<FP8, NT>(a.c, ks, kvh, lo, hi, wave, lane, a.n_new, scale, rows);
-    int at_lane = lane;
-    asm volatile("" : "+v"(at_lane));      // (those of the outputs: likewise)
-    const int at_row = at_lane & 15, at_group = at_lane >> 4;
-    join_waves<FP8, NT>(rows, lds, wave, at_lane,
-      [&](int qt, int c, f32x4 x, float l) {
-        const int r = 16 * qt + at_row;
-        if (r >= n_rows) return;
-        if (whole) {
-          const RowOf w = row_of(a, r);
-          uint16_t* out = row_at(a.o, a.so, s, kvh * a.group + w.head, w.token) + 32 * at_group + c;
-          const float by = l == 0.0f ? 0.0f : v_scale / l;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) out[8 * e] = __builtin_bit_cast(uint16_t, (__bf16)(l == 0.0f ? 0.0f : x[e] * by));
-        } else {
-          a.own_acc[((slot * 8 + c) * 4 + at_group) * n_rows + r] = x;
-        }
-      },
-      [&](int r, float ref, float l) {
-        if (r >= n_rows) return;
-        if (whole) {
-          const RowOf w = row_of(a, r);
-          if (a.lse) a.lse[((size_t)s * a.sq.heads + kvh * a.group + w.head) * a.n_new + w.token] = lse_of(ref, l);
-        } else {
-          a.own_sum[slot * n_rows + r] = make_float2(ref, l);
-        }
-      });
-    left -= count;
-    turn += count;
+    const int turns = turns_of(a.c, entry_at(a.c.lens, s)), from = turn - base, count = min(turns - from, left);
+    if (count > 0) {
+      if (from == 0 && tid == 0) a.turns[(size_t)kvh * a.n_seqs + s] = make_int2(base, all);
+      piece(s, from, count, count == turns && a.prefix_len == 0);
+      left -= count;
+      turn += count;
+    }
     base += turns;
   }
 }
@@ -617,40 +653,44 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void prefix_kernel(De
 #pragma unroll
   for (int qt = 0; qt < NT; ++qt) {
     const int row = min((tile * NT + qt) * 16 + n, a.n_seqs * n_rows - 1), s = row / n_rows;
-    load_row<FP8, NT>(a, kvh, s, row - s * n_rows, qt, g, rows);
+    load_row<FP8, NT>(a.q, a.sq, a.group, kvh, s, row - s * n_rows, qt, g, rows);
     rows.token[qt] = 0;
   }
   const Keys ks = {a.prefix_table, a.prefix_len, a.prefix_len, a.prefix_len - 1};
   const float scale = FP8 ? kLog2eByRootD * a.c.k_scale[kvh] : kLog2eByRootD;
-  int rest_from = lo;
+  int from = lo + kStep * wave;
   if constexpr (NT == 4) {
     // whole steps of pages that are there by the pipeline
     bool missing = false;
     for (int i = (lo >> a.c.page_shift) + lane; i <= (hi - 1) >> a.c.page_shift; i += 64) missing |= (unsigned)ks.table[i] >= (unsigned)a.c.n_pages;
-    const int first = lo + kStep * wave, whole = max(hi - first, 0) / kStep, steps = (whole + kWaves - 1) / kWaves;
+    const int steps = (max(hi - from, 0) / kStep + kWaves - 1) / kWaves & ~1;
     if (steps > 0 && __builtin_amdgcn_ballot_w64(missing) == 0) {
-      pipeline<FP8>(a.c, ks, kvh, first, steps, lane, scale, rows);
-      rest_from += steps * kTurn;
+      if (a.c.page_shift >= 5) pipeline<FP8, true>(a.c, ks, kvh, from, steps, lane, scale, rows);
+      else pipeline<FP8, false>(a.c, ks, kvh, from, steps, lane, scale, rows);
+      from += steps * kTurn;
     }
   }
-  sweep<FP8, NT>(a.c, ks, kvh, rest_from, hi, wave, lane, 1, scale, rows);
+  sweep<FP8, NT>(a.c, ks, kvh, from, hi, lane, 1, scale, rows);
   join_waves<FP8, NT>(rows, lds, wave, lane,
     [&](int qt, int c, f32x4 x, float) { a.pre_acc[((slot * 8 + c) * 4 + g) * (16 * NT) + 16 * qt + n] = x; },
     [&](int row, float ref, float l) { a.pre_sum[slot * 16 * NT + row] = make_float2(ref, l); });
 }
 
 // Joins the parts of 16 rows of a sequence and KV head.  The weights of the parts first, kMostWeights at a time, in LDS; then wave
-// (half, c) adds up the accumulators of number c of every other part, 4 loads in flight; the rows leave through LDS as whole ones.
+// (half, c) adds up the accumulators of number c of every part (HALVES = 2: of every other one), 4 loads in flight; the rows leave
+// through LDS as whole ones.
 constexpr int kMostWeights = 256;
-__global__ __launch_bounds__(1024) void join_kernel(DecodeArgs a, int pre_rows) {
+template <int HALVES>
+__global__ __launch_bounds__(512 * HALVES) void join_kernel(DecodeArgs a, int pre_rows) {
+  constexpr int kSeats = 32 * HALVES;      // parts whose weights are made at a time, 16 rows each
   __shared__ __attribute__((aligned(16))) uint16_t out[16][kHeadDim + 8];
-  __shared__ float weight[kMostWeights][16], most[64][16], sums[64][16];
-  __shared__ f32x4 half_acc[8][64];
+  __shared__ float weight[kMostWeights][16], most[kSeats][16], sums[kSeats][16];
+  __shared__ f32x4 half_acc[HALVES == 2 ? 8 : 1][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = wave & 7, half = wave >> 3;
   const int n = lane & 15, g = lane >> 4, n_rows = a.group * a.n_new;
   const int kvh = blockIdx.x % a.n_kvh, rest = blockIdx.x / a.n_kvh, tiles = (n_rows + 15) / 16, qt = rest % tiles, s = rest / tiles;
   const int r = min(16 * qt + n, n_rows - 1);
-  const int turns = turns_of(a.c, s);
+  const int turns = turns_of(a.c, entry_at(a.c.lens, s));
   int own_parts = 0;
   size_t own = 0;      // slot of the first part of the own keys
   if (turns > 0) {
@@ -667,18 +707,18 @@ __global__ __launch_bounds__(1024) void join_kernel(DecodeArgs a, int pre_rows) 
   auto sum_of = [&](int i) {
     return i < a.prefix_parts ? a.pre_sum[(pre + i) * pre_rows + in_tile] : a.own_sum[(own + i - a.prefix_parts) * n_rows + r];
   };
-  const int seat = tid >> 4;      // 64 parts at a time, 16 rows each (tid % 16 = n)
+  const int seat = tid >> 4;      // (tid % 16 = n)
   float top = kNoRef;
-  for (int i = seat; i < parts; i += 64) top = fmaxf(top, sum_of(i).x);
+  for (int i = seat; i < parts; i += kSeats) top = fmaxf(top, sum_of(i).x);
   most[seat][n] = top;
   __syncthreads();
-  for (int i = 0; i < min(64, parts); ++i) top = fmaxf(top, most[i][n]);
+  for (int i = 0; i < min(kSeats, parts); ++i) top = fmaxf(top, most[i][n]);
   float l = 0.0f;
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int i0 = 0; i0 < parts; i0 += kMostWeights) {
     const int here = min(kMostWeights, parts - i0);
     if (i0 > 0) __syncthreads();
-    for (int i = seat; i < (here + 7 & ~7); i += 64) {
+    for (int i = seat; i < (here + 7 & ~7); i += kSeats) {
       const float2 x = i < here ? sum_of(i0 + i) : make_float2(0.0f, 0.0f);
       // (a part without keys for this row has no accumulators)
       const float w = x.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(x.x - top);
@@ -686,42 +726,42 @@ __global__ __launch_bounds__(1024) void join_kernel(DecodeArgs a, int pre_rows) 
       if (x.y != 0.0f) l += w * x.y;
     }
     __syncthreads();
-    for (int i = half; i < here; i += 8) {
+    for (int i = half; i < here; i += 4 * HALVES) {
       f32x4 x[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int at = min(i0 + i + 2 * e, parts - 1), mine = at - a.prefix_parts;
+        const int at = min(i0 + i + HALVES * e, parts - 1), mine = at - a.prefix_parts;
         const f32x4* from = mine < 0 ? a.pre_acc + (((pre + at) * 8 + c) * 4 + g) * pre_rows + in_tile
                                      : a.own_acc + (((own + mine) * 8 + c) * 4 + g) * n_rows + r;
         x[e] = *from;
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float w = weight[i + 2 * e][n];
+        const float w = weight[i + HALVES * e][n];
 #pragma unroll
         for (int f = 0; f < 4; ++f) acc[f] += w == 0.0f ? 0.0f : w * x[e][f];
       }
     }
   }
   sums[seat][n] = l;
-  if (half == 1) half_acc[c][lane] = acc;
+  if (HALVES == 2 && half == 1) half_acc[c][lane] = acc;
   __syncthreads();
   if (half == 0) {
     l = 0.0f;
-    for (int i = 0; i < min(64, parts); ++i) l += sums[i][n];
-    acc += half_acc[c][lane];
+    for (int i = 0; i < min(kSeats, parts); ++i) l += sums[i][n];
+    if constexpr (HALVES == 2) acc += half_acc[c][lane];
     const float by = l == 0.0f ? 0.0f : (a.c.v_scale ? a.c.v_scale[kvh] : 1.0f) / l;
 #pragma unroll
     for (int e = 0; e < 4; ++e) out[n][32 * g + 8 * e + c] = __builtin_bit_cast(uint16_t, (__bf16)(l == 0.0f ? 0.0f : acc[e] * by));
     if (a.lse && c == 0 && g == 0 && 16 * qt + n < n_rows) {
-      const RowOf w = row_of(a, r);
+      const RowOf w = row_of(a.group, r);
       a.lse[((size_t)s * a.sq.heads + kvh * a.group + w.head) * a.n_new + w.token] = lse_of(top, l);
     }
   }
   __syncthreads();
   const int line = tid >> 4, r_out = 16 * qt + line;
   if (line < 16 && r_out < n_rows) {
-    const RowOf w = row_of(a, r_out);
+    const RowOf w = row_of(a.group, r_out);
     uint16_t* to = a.o + row_off(a.so, s * a.so.heads + kvh * a.group + w.head, w.token) + 8 * (tid & 15);
     *(u32x4*)to = *(const u32x4*)&out[line][8 * (tid & 15)];
   }
@@ -733,9 +773,11 @@ __global__ __launch_bounds__(1024) void join_kernel(DecodeArgs a, int pre_rows) 
 // 131072 keys: 266.8, 263.6, 268.9, 275.7, 291.9.  (More of them only read and write more partial results.  Cut into a number of
 // parts that each sequence had to itself, the first took 251 us: the longest sequences' parts ended last.)
 constexpr int kShares = 512;
+constexpr int kWholeTurns = 6;
 struct Plan {
   int own_tiles, pre_tiles;      // 16-row tiles per workgroup
   int shares, prefix_parts, prefix_chunk, row_tiles;
+  bool whole;                    // a workgroup per sequence and KV head, no workspace
   size_t pre_slots;
   size_t own_acc_bytes, own_sum_bytes, pre_acc_bytes, pre_sum_bytes, turns_bytes, bytes;
 };
@@ -749,13 +791,17 @@ Plan make_plan(const sale_params_t* p, const sale_cache_t* c, int prefix_len) {
   auto clamp = [](long long x, long long lo, long long hi) { return (int)(x < lo ? lo : x > hi ? hi : x); };
   w.own_tiles = tiles_for(n_rows);
   const long long turns = up((long long)c->table_width * c->page_tokens, kTurn) * p->batch;      // at most
-  w.shares = clamp(up(kShares, p->n_kv_heads), 1, turns);
+  w.whole = prefix_len == 0 && (long long)c->table_width * c->page_tokens <= kWholeTurns * kTurn;
+  w.shares = w.whole ? p->batch : clamp(up(kShares, p->n_kv_heads), 1, turns);
+  if (w.whole) return w;
   if (prefix_len > 0) {
     w.pre_tiles = tiles_for(all_rows);
     w.row_tiles = (int)up(all_rows, 16 * w.pre_tiles);
-    const long long groups = (long long)w.row_tiles * p->n_kv_heads;
-    const int parts = clamp(up(kShares, groups), 1, up(prefix_len, kTurn) < 128 ? up(prefix_len, kTurn) : 128);
-    w.prefix_chunk = (int)(up(up(prefix_len, parts), kTurn) * kTurn);
+    const long long groups = w.row_tiles * (long long)p->n_kv_heads;
+    const int parts = clamp(up(w.pre_tiles == 4 ? kShares / 2 : kShares, groups), 1,      // (64 rows: one workgroup per CU)
+                            up(prefix_len, kTurn) < 128 ? up(prefix_len, kTurn) : 128);
+    const int whole = w.pre_tiles == 4 ? 2 * kTurn : kTurn;      // (the pipeline takes steps by two)
+    w.prefix_chunk = (int)(up(up(prefix_len, parts), whole) * whole);
     w.prefix_parts = (int)up(prefix_len, w.prefix_chunk);
     w.pre_slots = (size_t)groups * w.prefix_parts;
   }
@@ -791,11 +837,20 @@ void launch_decode(const DecodeArgs& a, const Plan& w, hipStream_t st) {
     else if (w.pre_tiles == 2) prefix_kernel<FP8, 2><<<pre, threads, 0, st>>>(a);
     else prefix_kernel<FP8, 4><<<pre, threads, 0, st>>>(a);
   }
-  if (w.own_tiles == 1) own_kernel<FP8, 1><<<own, threads, 0, st>>>(a);
-  else if (w.own_tiles == 2) own_kernel<FP8, 2><<<own, threads, 0, st>>>(a);
-  else own_kernel<FP8, 4><<<own, threads, 0, st>>>(a);
+  if (w.whole) {
+    if (w.own_tiles == 1) own_kernel<FP8, 1, true><<<own, threads, 0, st>>>(a);
+    else if (w.own_tiles == 2) own_kernel<FP8, 2, true><<<own, threads, 0, st>>>(a);
+    else own_kernel<FP8, 4, true><<<own, threads, 0, st>>>(a);
+    return;
+  }
+  if (w.own_tiles == 1) own_kernel<FP8, 1, false><<<own, threads, 0, st>>>(a);
+  else if (w.own_tiles == 2) own_kernel<FP8, 2, false><<<own, threads, 0, st>>>(a);
+  else own_kernel<FP8, 4, false><<<own, threads, 0, st>>>(a);
   const int n_rows = a.group * a.n_new, tiles = (n_rows + 15) / 16;
-  join_kernel<<<dim3((unsigned)((size_t)a.n_seqs * a.n_kvh * tiles)), dim3(1024), 0, st>>>(a, 16 * (w.pre_tiles > 0 ? w.pre_tiles : 1));
+  const dim3 join((unsigned)((size_t)a.n_seqs * a.n_kvh * tiles));
+  const int pre_rows = 16 * (w.pre_tiles > 0 ? w.pre_tiles : 1);
+  if (join.x > kShares) join_kernel<1><<<join, dim3(512), 0, st>>>(a, pre_rows);      // (more of them than fit at a time: small ones)
+  else join_kernel<2><<<join, dim3(1024), 0, st>>>(a, pre_rows);
 }
 
 }  // namespace
@@ -816,7 +871,7 @@ extern "C" int sale_decode_attn(const sale_params_t* p, const sale_cache_t* cach
   if (rc != SALE_OK) return rc;
   if (((uintptr_t)q | (uintptr_t)o) & 15) return SALE_ERR_BAD_SHAPE;
   const Plan w = make_plan(p, cache, prefix_len);
-  if (!ws || ws_bytes < w.bytes || ((uintptr_t)ws & 15)) return SALE_ERR_WORKSPACE;
+  if (w.bytes > 0 && (!ws || ws_bytes < w.bytes || ((uintptr_t)ws & 15))) return SALE_ERR_WORKSPACE;
   DecodeArgs a = {};
   a.c = cache_view(p, cache);
   if (cache->dtype != SALE_PAGE_FP8) a.c.k_scale = a.c.v_scale = nullptr;

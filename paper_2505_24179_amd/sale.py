@@ -170,6 +170,7 @@ class Cache:
             if t is not None and t.device != self.k.device:
                 raise ValueError(f"{name}: on {t.device}, the pages of K on {self.k.device}")
 
+    # What follows from shapes and strides is made once; the addresses are read by every call.
     @cached_property
     def _struct(self):
         c = _Cache(n_pages=self.k.shape[0], page_tokens=self.k.shape[2], table_width=self.table.shape[1],
@@ -177,20 +178,21 @@ class Cache:
         for name, t in (("k_stride", self.k), ("v_stride", self.v)):
             if not t.is_contiguous():
                 getattr(c, name)[:] = t.stride()[:3]
-        return c
+        return c, self.k.shape[1], self.k.shape[3], self.table.shape[0], self.k.get_device(), (self.k.shape[2], self.table.shape[1])
 
     def _arg(self, p: "Params", sequences=None):
-        """The C struct, as an argument of a call with parameters p (over so many sequences)."""
-        shape = self.k.shape
-        if shape[1] != p.n_kv_heads or shape[3] != p.head_dim:
-            raise ValueError(f"cache: pages of {shape[1]} KV heads x {shape[3]} channels, the call has {p.n_kv_heads} x {p.head_dim}")
-        if sequences is not None and self.table.shape[0] != sequences:
-            raise ValueError(f"cache: a table of {self.table.shape[0]} sequences, the call has {sequences}")
-        c = self._struct
+        """The C struct for a call with parameters p (over so many sequences)."""
+        c, heads, head_dim, rows, device, _ = self._struct
+        if heads != p.n_kv_heads or head_dim != p.head_dim:
+            raise ValueError(f"cache: pages of {heads} KV heads x {head_dim} channels, the call has {p.n_kv_heads} x {p.head_dim}")
+        if sequences is not None and rows != sequences:
+            raise ValueError(f"cache: a table of {rows} sequences, the call has {sequences}")
+        if device != torch._C._cuda_getDevice():
+            raise ValueError(f"cache: expected pages on the current device, got {self.k.device}")
         c.k, c.v, c.table, c.lens = self.k.data_ptr(), self.v.data_ptr(), self.table.data_ptr(), self.lens.data_ptr()
         if c.dtype == PAGE_FP8:
             c.k_scale, c.v_scale = self.k_scale.data_ptr(), self.v_scale.data_ptr()
-        return ctypes.byref(c)
+        return c
 
 
 _vp, _sz, _i32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32
@@ -486,12 +488,12 @@ def calibrate_tau(p: Params, q, k, v, tau0: float = 0.008, theta: float = 0.4, m
     return tau, err, halv
 
 
-def _on_current_device(**tensors):
+def _on_current_device(names: str, *tensors):
     """The calls are launched on the current device's stream."""
     at = torch._C._cuda_getDevice()
-    for name, t in tensors.items():
+    for i, t in enumerate(tensors):
         if t is not None and t.get_device() != at:
-            raise ValueError(f"{name}: expected a tensor on the current device, cuda:{at}, got {t.device}")
+            raise ValueError(f"{names.split()[i]}: expected a tensor on the current device, cuda:{at}, got {t.device}")
 
 
 def _n_sequences(p: Params) -> int:
@@ -506,7 +508,7 @@ def prompt_attn(p: Params, q, k, v, want_lse: bool = False, out=None, ws=None):
     lse = torch.empty(p.batch, p.n_q_heads, p.seq_len, dtype=torch.float32, device=q.device) if want_lse else None
     if ws is None:
         ws = torch.empty(max(1, workspace_bytes(p, WS_PROMPT_ATTN)), dtype=torch.uint8, device=q.device)
-    _on_current_device(q=q, k=k, v=v, out=o, ws=ws)
+    _on_current_device("q k v out workspace", q, k, v, o, ws)
     _check(_lib.sale_prompt_attn(args, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(ws), _expect_ws(ws), _stream()))
     return o, lse
 
@@ -516,7 +518,7 @@ def cache_append(p: Params, cache: Cache, k, v) -> None:
     as the last n of the cache.lens[s] tokens that it holds with them."""
     c = cache._arg(p, _n_sequences(p))
     args = _args(p, k=k, v=v)
-    _on_current_device(cache=cache.k, k=k, v=v)
+    _on_current_device("k v", k, v)
     _check(_lib.sale_cache_append(args, c, _ptr(k), _ptr(v), _stream()))
 
 
@@ -535,12 +537,15 @@ def cache_copy(p: Params, cache: Cache, src, dst) -> None:
     if src.numel() != dst.numel():
         raise ValueError(f"cache_copy: {src.numel()} sources, {dst.numel()} destinations")
     c = cache._arg(p)
-    _on_current_device(cache=cache.k)
     _check(_lib.sale_cache_copy(p._contiguous, c, _ptr(src), _ptr(dst), src.numel(), _stream()))
 
 
 def decode_workspace_bytes(p: Params, cache: Cache, prefix_len: int = 0) -> int:
-    return int(_lib.sale_decode_workspace_bytes(p._contiguous, cache._arg(p, _n_sequences(p)), prefix_len))
+    key = (*cache._struct[5], prefix_len)
+    n = p._ws_bytes.get(key)
+    if n is None:
+        n = p._ws_bytes[key] = int(_lib.sale_decode_workspace_bytes(p._contiguous, cache._arg(p, _n_sequences(p)), prefix_len))
+    return n
 
 
 def decode_attn(p: Params, cache: Cache, q, prefix=None, prefix_len: int = 0, want_lse: bool = False, out=None, ws=None):
@@ -558,7 +563,11 @@ def decode_attn(p: Params, cache: Cache, q, prefix=None, prefix_len: int = 0, wa
         prefix = None
     lse = torch.empty(p.batch, p.n_q_heads, p.seq_len, dtype=torch.float32, device=q.device) if want_lse else None
     if ws is None:
-        ws = torch.empty(max(1, _lib.sale_decode_workspace_bytes(args, c, prefix_len)), dtype=torch.uint8, device=q.device)
-    _on_current_device(cache=cache.k, q=q, prefix=prefix, out=o, ws=ws)
-    _check(_lib.sale_decode_attn(args, c, _ptr(q), _ptr(prefix), prefix_len, _ptr(o), _ptr(lse), _ptr(ws), _expect_ws(ws), _stream()))
+        n_ws = decode_workspace_bytes(p, cache, prefix_len)
+        if n_ws:
+            ws = torch.empty(n_ws, dtype=torch.uint8, device=q.device)
+    else:
+        n_ws = _expect_ws(ws)
+    _on_current_device("q prefix out workspace", q, prefix, o, ws)
+    _check(_lib.sale_decode_attn(args, c, _ptr(q), _ptr(prefix), prefix_len, _ptr(o), _ptr(lse), _ptr(ws), n_ws, _stream()))
     return o, lse

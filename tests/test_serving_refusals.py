@@ -63,7 +63,7 @@ BAD_CACHE = [(dict(k=None), -1), (dict(v=None), -1), (dict(table=None), -1), (di
              (dict(table_width=0), -2), (dict(page_tokens=0), -2), (dict(page_tokens=8), -3), (dict(page_tokens=48), -3),
              (dict(page_tokens=512), -3), (dict(dtype=2), -3), (dict(dtype=1), -1), (dict(dtype=1, k_scale=0x1000), -1),
              (dict(k=0x1008), -2), (dict(v=0x1002), -2), (dict(k_stride=(4096, 2048, 64)), -2), (dict(v_stride=(4096, 2048, 132)), -2),
-             (dict(k_stride=(4096, 0, 128)), -2), (dict(v_stride=(0, 2048, 128)), -2), (dict(k_stride=(4096, 2048, 1 << 25)), -2),
+             (dict(k_stride=(4096, 0, 128)), -2), (dict(v_stride=(0, 2048, 128)), -2), (dict(k_stride=(4096, 2048, (1 << 22) + 8)), -3), (dict(v_stride=(1 << 31, 2048, 128)), -3),
              (dict(k_stride=(-4096, 2048, 128)), -2), (dict(dtype=1, k_scale=0x1000, v_scale=0x1000, k_stride=(4096, 2048, 136)), -2),
              (dict(table_width=1 << 28), -3)]
 
