@@ -162,9 +162,9 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
 }
 
 // O += V p of one key, for the rows that see it.  (Rare, see step: V comes from the page again.)
-template <bool FP8, int NT>
-__device__ __forceinline__ void one_key(const CacheView& c, Rows<FP8, NT>& rows, const bf16x8 (&p)[NT], const Keys& ks, int kvh, int key,
-                                        int key0, TwoPages pg, int g) {
+template <bool FP8, int NT, bool FINE>
+__device__ __forceinline__ void one_key(const CacheView& c, Rows<FP8, NT>& rows, const bf16x8 (&p)[NT], const bf16x8 (&rest)[FINE ? NT : 1],
+                                        const Keys& ks, int kvh, int key, int key0, TwoPages pg, int g) {
   const int in = key - key0, page = in < 16 ? pg.a : pg.b;
   if (page < 0) return;
   const uint8_t* v = c.v.base + (long long)page * c.v.page + (long long)kvh * c.v.head +
@@ -175,7 +175,7 @@ __device__ __forceinline__ void one_key(const CacheView& c, Rows<FP8, NT>& rows,
     float x = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (j == in >> 2) x = (float)p[qt][j];
+      if (j == in >> 2) x = FINE ? (float)p[qt][j] + (float)rest[FINE ? qt : 0][j] : (float)p[qt][j];
     pk[qt] = __shfl(x, (int)(threadIdx.x & 15) + 16 * (in & 3), 64);
   }
 #pragma unroll
@@ -194,8 +194,11 @@ __device__ __forceinline__ void one_key(const CacheView& c, Rows<FP8, NT>& rows,
   }
 }
 
-// One step: its 32 keys enter acc, l and ref.  edge: some of the keys are not there, or not for all rows.
-template <bool FP8, int NT>
+// One step: its 32 keys enter acc, l and ref.  edge: some of the keys are not there, or not for all rows.  FINE: the probabilities
+// enter as two bf16 each, the leading bits and the rest: where reading the keys is what takes the time, the second product and
+// its operands cost nothing that shows, and O is then off by its own rounding alone.  (Where the registers suffice: not for the
+// own keys of 17 rows and more, nor for 64 rows of the prefix, where the matrix unit is what takes the time.)
+template <bool FP8, int NT, bool FINE>
 __device__ __forceinline__ void step(const CacheView& c, Operands<FP8>& x, Rows<FP8, NT>& rows, float scale, const Keys& ks, int kvh,
                                      int key0, TwoPages pg, bool edge, int g, int n_new) {
   f32x4 S[2][NT];
@@ -225,7 +228,7 @@ __device__ __forceinline__ void step(const CacheView& c, Operands<FP8>& x, Rows<
         if (!page || key >= min(ks.before + rows.token[qt] + 1, ks.n)) S[j >> 2][qt][j & 3] = -INFINITY;
     }
   }
-  bf16x8 p[NT];
+  bf16x8 p[NT], rest[FINE ? NT : 1];
 #pragma unroll
   for (int qt = 0; qt < NT; ++qt) {
     float v[8];
@@ -246,9 +249,20 @@ __device__ __forceinline__ void step(const CacheView& c, Operands<FP8>& x, Rows<
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float e = __builtin_amdgcn_exp2f(v[j] - rows.ref[qt]);
-      rows.l[qt] += e;
-      p[qt][j] = (__bf16)e;
+      v[j] = __builtin_amdgcn_exp2f(v[j] - rows.ref[qt]);
+      rows.l[qt] += v[j];
+    }
+    if constexpr (FINE) {
+      u32x4 w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, v[2 * i + 1]), __builtin_bit_cast(uint32_t, v[2 * i]), 0x07060302u);
+      p[qt] = __builtin_bit_cast(bf16x8, w);
+      // (never 0 or negative beside a p that is not 0: an infinity of V stays what it is)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) rest[qt][j] = (__bf16)__builtin_fmaf((float)p[qt][j], 0x1p-20f, v[j] - (float)p[qt][j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p[qt][j] = (__bf16)v[j];
     }
   }
   if (edge) {
@@ -271,19 +285,22 @@ __device__ __forceinline__ void step(const CacheView& c, Operands<FP8>& x, Rows<
 #pragma unroll
         for (int e = 0; e < (FP8 ? 2 : 4); ++e)
           if (key0 + 16 * (j >> 2) + 4 * (j & 3) + g >= ks.all) x.v[j][e] = 0;
-      for (int key = max(ks.all, key0); key < min(ks.n, key0 + kStep); ++key) one_key<FP8, NT>(c, rows, p, ks, kvh, key, key0, pg, g);
+      for (int key = max(ks.all, key0); key < min(ks.n, key0 + kStep); ++key) one_key<FP8, NT, FINE>(c, rows, p, rest, ks, kvh, key, key0, pg, g);
     }
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const bf16x8 v = turned<FP8>(x, e);
 #pragma unroll
-    for (int qt = 0; qt < NT; ++qt) rows.acc[qt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[qt], rows.acc[qt][e], 0, 0, 0);
+    for (int qt = 0; qt < NT; ++qt) {
+      rows.acc[qt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[qt], rows.acc[qt][e], 0, 0, 0);
+      if constexpr (FINE) rows.acc[qt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, rest[qt], rows.acc[qt][e], 0, 0, 0);
+    }
   }
 }
 
 // Keys from .. hi - 1 for the rows, 32 of every kTurn.
-template <bool FP8, int NT>
+template <bool FP8, int NT, bool FINE>
 __device__ __forceinline__ void sweep(const CacheView& c, const Keys& ks, int kvh, int from, int hi, int lane, int n_new, float scale,
                                       Rows<FP8, NT>& rows) {
   const LaneOffsets at = lane_offsets<FP8>(c, lane);
@@ -291,7 +308,7 @@ __device__ __forceinline__ void sweep(const CacheView& c, const Keys& ks, int kv
     const TwoPages pg = pages_of(c, ks, key0);
     Operands<FP8> x;
     load_step<FP8>(c, ks, kvh, key0, pg, at, x);
-    step<FP8, NT>(c, x, rows, scale, ks, kvh, key0, pg, key0 + kStep > ks.all || (pg.a | pg.b) < 0, lane >> 4, n_new);
+    step<FP8, NT, FINE>(c, x, rows, scale, ks, kvh, key0, pg, key0 + kStep > ks.all || (pg.a | pg.b) < 0, lane >> 4, n_new);
   }
 }
 
@@ -584,7 +601,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void own_kernel(Decod
     for (int qt = 0; qt < NT; ++qt)
       load_row<FP8, NT>(args->q, sq, a.group, kvh, s, min(16 * qt + (from_lane & 15), n_rows - 1), qt, from_lane >> 4, rows);
     const Keys ks = {a.c.table + (size_t)s * a.c.width, n_keys, min(held - a.n_new + 1, n_keys), held - a.n_new};
-    sweep<FP8, NT>(a.c, ks, kvh, lo + kStep * wave, hi, from_lane, a.n_new, scale, rows);
+    sweep<FP8, NT, NT == 1>(a.c, ks, kvh, lo + kStep * wave, hi, from_lane, a.n_new, scale, rows);
     int at_lane = from_lane;
     auto late = (const __attribute__((address_space(4))) DecodeArgs*)__builtin_amdgcn_kernarg_segment_ptr();
     asm volatile("" : "+v"(at_lane), "+s"(late));
@@ -670,7 +687,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void prefix_kernel(De
       from += steps * kTurn;
     }
   }
-  sweep<FP8, NT>(a.c, ks, kvh, from, hi, lane, 1, scale, rows);
+  sweep<FP8, NT, NT != 4>(a.c, ks, kvh, from, hi, lane, 1, scale, rows);
   join_waves<FP8, NT>(rows, lds, wave, lane,
     [&](int qt, int c, f32x4 x, float) { a.pre_acc[((slot * 8 + c) * 4 + g) * (16 * NT) + 16 * qt + n] = x; },
     [&](int row, float ref, float l) { a.pre_sum[slot * 16 * NT + row] = make_float2(ref, l); });

@@ -85,6 +85,22 @@ def test_a_new_token_does_not_reach_those_before_it(sale, kind, page, value):
             assert torch.isnan(o[s, :, n - back:, 0:128:3]).all()
 
 
+@pytest.mark.parametrize("hq,prefix_len", [(4, 0), (4, 40), (24, 0), (40, 200)])
+def test_infinite_values_that_are_seen(sale, hq, prefix_len):
+    """An infinity in V is one in O, of its sign, whatever the probability's last bits are; one of each sign is NaN."""
+    gen = torch.Generator().manual_seed(16)
+    cache, prefix = make_cache(sale, [70, 45, 130], 1, 16, "bf16", "bhnd", gen, prefix_len, spoil=False)
+    v = cache.v
+    v[int(cache.table[0, 1]), 0, 3, 7], v[int(cache.table[0, 1]), 0, 4, 8] = float("inf"), -float("inf")
+    v[int(cache.table[1, 0]), 0, 5, 9] = v[int(cache.table[1, 2]), 0, 2, 9] = float("inf")
+    v[int(cache.table[2, 0]), 0, 5, 9], v[int(cache.table[2, 7]), 0, 0, 9] = float("inf"), -float("inf")
+    q = rows((3, hq, 1, 128), "bhnd", gen, 0.5)
+    q[0] = 0      # (all probabilities equal)
+    o, lse = sale.decode_attn(sale.Params(3, hq, 1, 1), cache, q, prefix=prefix, prefix_len=prefix_len, want_lse=True)
+    check(o, lse, decode_oracle(cache, q, prefix, prefix_len))
+    assert bool((o[0, :, 0, 7] == float("inf")).all() and (o[0, :, 0, 8] == -float("inf")).all() and torch.isnan(o[2, :, 0, 9]).all())
+
+
 def test_a_query_that_is_not_finite_stays_alone(sale):
     gen = torch.Generator().manual_seed(9)
     cache, prefix = make_cache(sale, [50, 60, 70], 1, 16, "bf16", "bhnd", gen, 40)
