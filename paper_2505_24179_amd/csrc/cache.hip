@@ -53,7 +53,9 @@ namespace {
 // A workgroup takes up to `tile` tokens of one sequence, all KV heads, K and V: 16 bytes (8 channels) of the new token per
 // thread and turn, so that a row of 256 bytes is 16 neighbouring threads'.  Where the tokens of a sequence lie among the
 // packed ones travels with the launch, up to kAppendChunk sequences at a time.
-constexpr int kAppendChunk = 255;
+// 24433 tokens of 8 heads into 8-bit pages (150 MB in and out) with 16, 32, 64, 128, 256 rows per workgroup: 47.4, 37.7, 42.0, 39.0,
+// 55.8 us.
+constexpr int kAppendChunk = 255, kAppendRows = 32;
 struct AppendJob {
   CacheView c;
   const uint8_t *k, *v;
@@ -66,15 +68,16 @@ struct AppendJob {
 
 // e4m3(x / scale), nearest, ties to even; at most 448 in size; NaN stays.  The quotient is the correctly rounded one: with
 // inv = 1 / scale correctly rounded, q = x inv is next to it and one step of Newton's with the exact remainder gives it (Markstein,
-// 1990), in 3 instructions where the compiler's division takes 10.  Quotients of 1000 and more are only limited; a scale so far
-// out that remainders could leave the range of a float takes the division.
+// 1990), in 3 instructions where the compiler's division takes 10.  (q is limited first: from an infinite one the step would make a
+// NaN; what is limited there is limited in the end.)  A scale so far out that remainders could leave the range of a float takes
+// the division.
 struct Divisor { float scale, inv; bool far; };
 __device__ __forceinline__ Divisor divisor(float scale) { return {scale, 1.0f / scale, !(scale >= 0x1p-60f && scale <= 0x1p60f)}; }
 __device__ __forceinline__ float quotient448(float x, const Divisor& d) {
-  float q = x * d.inv;
-  if (d.far) q = x / d.scale;
-  else if (__builtin_fabsf(q) < 1000.0f) q = __builtin_fmaf(__builtin_fmaf(-q, d.scale, x), d.inv, q);
-  return q != q ? q : __builtin_amdgcn_fmed3f(q, -448.0f, 448.0f);
+  float q = __builtin_amdgcn_fmed3f(x * d.inv, -1000.0f, 1000.0f);
+  q = __builtin_fmaf(__builtin_fmaf(-q, d.scale, x), d.inv, q);
+  if (__builtin_expect(d.far, 0)) q = x / d.scale;
+  return __builtin_elementwise_minimum(__builtin_elementwise_maximum(q, -448.0f), 448.0f);      // (a NaN passes these)
 }
 __device__ __forceinline__ u32x2 to_fp8(u32x4 w, const Divisor& d) {
   u32x2 out;
@@ -117,6 +120,10 @@ __global__ __launch_bounds__(256) void append_kernel(AppendJob a) {
   const int start = max(a.c.lens[s], 0) - n_new;      // position of the sequence's first new token
   const int32_t* table = a.c.table + (size_t)s * a.c.width;
   const int batch = a.each > 0 ? s : 0;
+  // Rows come in lines: the heads of a token, or the tokens of a head.  (More than one token: 64 rows at most, and the product with
+  // 2^16 / line_rows, rounded up, divides them exactly.)
+  const bool by_head = a.heads_first || a.tile == 1;
+  const int line_rows = by_head ? a.n_kvh : count, per_line = a.tile == 1 ? 0 : (65535 + line_rows) / line_rows;
   // (four turns at a time: their page numbers and tokens are in flight together)
   for (int id0 = threadIdx.x; id0 < 2 * rows * 16; id0 += 4 * 256) {
     u32x4 w[4];
@@ -126,13 +133,15 @@ __global__ __launch_bounds__(256) void append_kernel(AppendJob a) {
       const int id = min(id0 + 256 * u, 2 * rows * 16 - 1);
       const bool is_v = id >= rows * 16;
       const int row = (is_v ? id - rows * 16 : id) >> 4;
-      const int h = a.heads_first ? row % a.n_kvh : row / count, i = a.heads_first ? row / a.n_kvh : row % count;
+      const int line = row * per_line >> 16, in_line = row - line * line_rows;
+      const int h = by_head ? in_line : line, i = by_head ? line : in_line;
       head[u] = h;
       pos[u] = start + t0 + i;
       const bool place = pos[u] >= 0 && pos[u] >> a.c.page_shift < a.c.width && id0 + 256 * u < 2 * rows * 16;
       page[u] = place ? table[pos[u] >> a.c.page_shift] : -1;
       const Strided& ss = is_v ? a.sv : a.sk;
-      w[u] = *(const u32x4*)((is_v ? a.v : a.k) + 2 * ((size_t)batch * ss.sb + (size_t)h * ss.sh + (size_t)(first + t0 + i) * ss.st) + 16 * (id & 15));
+      w[u] = __builtin_nontemporal_load((const u32x4*)(
+          (is_v ? a.v : a.k) + 2 * ((size_t)batch * ss.sb + (size_t)h * ss.sh + (size_t)(first + t0 + i) * ss.st) + 16 * (id & 15)));
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -149,10 +158,11 @@ __global__ __launch_bounds__(256) void append_kernel(AppendJob a) {
 }
 
 // ---- copy --------------------------------------------------------------------------------------------------
-// Pairs of pages travel with the launch, kCopyChunk at a time.  A workgroup copies 16 KB of K or of V, 4 loads of 16 bytes
-// per thread in flight.
-constexpr int kCopyChunk = 448;
-constexpr int kCopyBytes = 16384;
+// Pairs of pages travel with the launch, kCopyChunk at a time.  A workgroup copies kCopyLoads x 4 KB of K or of V; what it reads and
+// writes passes the caches by.  1021 pages of 256 KB (535 MB read and written): 100 us, 5.3 TB/s; with loads and stores that do not
+// 108, with 16 KB per workgroup 118 and 108.
+constexpr int kCopyChunk = 448, kCopyLoads = 2;
+constexpr int kCopyBytes = kCopyLoads * 4096;
 struct CopyJob {
   PageSide k, v;
   int parts;              // workgroups per page and side
@@ -169,18 +179,18 @@ __global__ __launch_bounds__(256) void copy_kernel(CopyJob a) {
   uint8_t* to = side.base + (long long)a.dst[pair] * side.page;
   const int pieces = a.n_kvh << (a.page_shift + a.row_shift), tokens = 1 << a.page_shift;
   const int first = (part < a.parts ? part : part - a.parts) * (kCopyBytes / 16) + (int)threadIdx.x;
-  u32x4 w[4];
-  long long at[4];
+  u32x4 w[kCopyLoads];
+  long long at[kCopyLoads];
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
+  for (int r = 0; r < kCopyLoads; ++r) {
     const int piece = first + 256 * r, row = piece >> a.row_shift;
     const int h = a.heads_first ? row % a.n_kvh : row >> a.page_shift, slot = a.heads_first ? row / a.n_kvh : row & (tokens - 1);
     at[r] = (long long)h * side.head + (long long)slot * side.token + 16 * (piece & ((1 << a.row_shift) - 1));
-    if (piece < pieces) w[r] = *(const u32x4*)(from + at[r]);
+    if (piece < pieces) w[r] = __builtin_nontemporal_load((const u32x4*)(from + at[r]));
   }
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
-    if (first + 256 * r < pieces) *(u32x4*)(to + at[r]) = w[r];
+  for (int r = 0; r < kCopyLoads; ++r)
+    if (first + 256 * r < pieces) __builtin_nontemporal_store(w[r], (u32x4*)(to + at[r]));
 }
 
 // All pages in range, the destinations different and none a source.  (One bit per page in each of two sets; < 0: SALE_ERR_*)
@@ -222,7 +232,7 @@ extern "C" int sale_cache_append(const sale_params_t* p, const sale_cache_t* cac
   a.sv = layout_of(p->v_stride, p->n_kv_heads, p->seq_len);
   a.n_kvh = p->n_kv_heads;
   a.heads_first = a.sk.sh < a.sk.st ? 1 : 0;
-  a.tile = 64 / p->n_kv_heads < 1 ? 1 : 64 / p->n_kv_heads;      // 8 turns of a workgroup
+  a.tile = kAppendRows / p->n_kv_heads < 1 ? 1 : kAppendRows / p->n_kv_heads;
   const hipStream_t st = (hipStream_t)stream;
   auto launch = [&](long long workgroups) -> int {
     if (workgroups > 0x7FFFFFFF) return SALE_ERR_UNSUPPORTED;
