@@ -128,14 +128,36 @@ struct OrderJob {
 // Without the copy of K the first pass over the 8-bit operands follows in the same launch, from workgroup `tiles` on.
 struct Then8 { int tiles; Pass8 pass; };
 struct NoPass8 {};
-// ODD: sequences of any length (Geo::tokens_of).  Behind a sequence's last token V' is zero and K' repeats its last key (which
-// only queries behind it would see).
+// Sequences of any length (see sale_prompt_attn): the row blocks of up to kTokenChunk of them, which travel with the launch.
+constexpr int kTokenChunk = 255;
+struct TokenChunk {
+  int n;
+  int block[kTokenChunk + 1];      // first block of every sequence of the chunk, and the end of the last
+  int token[kTokenChunk + 1];      // first token, likewise
+  __device__ int sequence_of(int b) const {      // the last sequence that starts at block b or before: the one that has it
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (block[mid] <= b) lo = mid; else hi = mid;
+    }
+    return lo;
+  }
+  __device__ int2 tokens_of(int s, int b) const {      // first token of block b of sequence s, and how many it has
+    const int t = token[s] + 64 * (b - block[s]);
+    return make_int2(t, min(64, token[s + 1] - t));
+  }
+};
+struct NoChunk {};
+// ODD: sequences of any length, the blocks of one chunk.  Behind a sequence's last token V' is zero and K' repeats its last key
+// (which only queries behind it would see).  The workgroups of the first KV head write down what the attention kernel needs to
+// know of a block, unless rows are sorted here, which needs it before.
 template <bool K, bool V, bool ODD = false>
 __global__ __launch_bounds__(256) void rearrange_kv_kernel(Geo g, OrderJob job, std::conditional_t<K, NoPass8, Then8> then,
                                                            const uint16_t* __restrict__ k,
                                                            const uint16_t* __restrict__ v,
                                                            u32x4* __restrict__ kp, u32x4* __restrict__ vp,
-                                                           int* __restrict__ slot_counter) {
+                                                           int* __restrict__ slot_counter,
+                                                           std::conditional_t<ODD, TokenChunk, NoChunk> chunk) {
   __shared__ union { uint16_t sv[64 * (kHeadDim + 2)]; int bin[kOrderBins]; double pass[128]; } lds;
   if ((int)blockIdx.x < job.heads) {
     if (job.taken && threadIdx.x == 0) job.taken[kQueueStride * blockIdx.x] = 0;
@@ -149,15 +171,27 @@ __global__ __launch_bounds__(256) void rearrange_kv_kernel(Geo g, OrderJob job, 
   const Strided &lk = g.sk, &lv = g.sv;
   const int tid = threadIdx.x;
   if (slot_counter && block == 0 && tid == 0) *slot_counter = 0;      // (for order_units_kernel, next on the stream)
-  const size_t tile = block;                           // flattened (kv head, block j): rows tile*64 .. +63
+  size_t tile = block;                                 // flattened (kv head, block j): rows tile*64 .. +63
   const int tiles_per_head = seq / 64;
-  const int2 part = ODD ? g.tokens_of[tile % tiles_per_head] : make_int2((int)(tile % tiles_per_head) * 64, 64);
-  const uint16_t* kt = k + row_off(lk, (int)(tile / tiles_per_head), part.x);
-  const uint16_t* vt = v + row_off(lv, (int)(tile / tiles_per_head), part.x);
+  int kvh = (int)(tile / tiles_per_head);
+  int2 part = make_int2((int)(tile % tiles_per_head) * 64, 64);
+  if constexpr (ODD) {
+    const int here = chunk.block[chunk.n] - chunk.block[0];
+    kvh = block / here;
+    const int j = chunk.block[0] + block % here, s = chunk.sequence_of(j);
+    part = chunk.tokens_of(s, j);
+    tile = (size_t)kvh * tiles_per_head + j;
+    if (kvh == 0 && tid == 0 && job.heads == 0) {
+      const_cast<int32_t*>(g.seq_start)[j] = chunk.block[s];
+      const_cast<int2*>(g.tokens_of)[j] = part;
+    }
+  }
+  const uint16_t* kt = k + row_off(lk, kvh, part.x);
+  const uint16_t* vt = v + row_off(lv, kvh, part.x);
 #pragma unroll
   for (int r = 0; r < (V ? 4 : 0); ++r) {
-    const int chunk = tid + 256 * r;                   // V tile -> LDS, rows padded by one bank
-    const int row = chunk >> 4, col = (chunk & 15) * 8;
+    const int piece = tid + 256 * r;                   // V tile -> LDS, rows padded by one bank
+    const int row = piece >> 4, col = (piece & 15) * 8;
     u32x4 w = {0, 0, 0, 0};
     if (!ODD || row < part.y) w = *(const u32x4*)(vt + (size_t)row * lv.st + col);
     uint32_t* d = (uint32_t*)&sv[row * (kHeadDim + 2) + col];
@@ -1477,7 +1511,7 @@ int launch_attn_rows(const sale_params_t* p, const void* q, const void* k, const
   const int tiles = pv8 ? (w.slot_counter ? 1 : 0) : g.n_kvh * (g.seq / 64);
   const dim3 first((unsigned)(job.heads + tiles + pass.blocks()));
   const Then8 then = {tiles, pass};
-#define SALE_REARRANGE_ARGS (const uint16_t*)k, (const uint16_t*)v, kp, vp, w.slot_counter
+#define SALE_REARRANGE_ARGS (const uint16_t*)k, (const uint16_t*)v, kp, vp, w.slot_counter, NoChunk{}
   if (!qk8) rearrange_kv_kernel<true, true><<<first, dim3(256), 0, st>>>(g, job, NoPass8{}, SALE_REARRANGE_ARGS);
   else if (!pv8) rearrange_kv_kernel<false, true><<<first, dim3(256), 0, st>>>(g, job, then, SALE_REARRANGE_ARGS);
   else rearrange_kv_kernel<false, false><<<first, dim3(256), 0, st>>>(g, job, then, SALE_REARRANGE_ARGS);
@@ -1511,24 +1545,12 @@ int launch_attn_rows(const sale_params_t* p, const void* q, const void* k, const
 // are addressed by token, and what is not finite in V is kept from queries before its key (key_by_key).
 namespace {
 
-constexpr int kTokenChunk = 255;
-struct TokenChunk {
-  int n;
-  int block[kTokenChunk + 1];      // first block of every sequence of the chunk, and the end of the last
-  int token[kTokenChunk + 1];      // first token, likewise
-};
-
 __global__ __launch_bounds__(256) void token_table_kernel(TokenChunk c, int32_t* __restrict__ seq_start, int2* __restrict__ tokens_of) {
   const int b = c.block[0] + blockIdx.x * 256 + threadIdx.x;
   if (b >= c.block[c.n]) return;
-  int lo = 0, hi = c.n;      // the last sequence that starts at block b or before: the one that has it
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (c.block[mid] <= b) lo = mid; else hi = mid;
-  }
-  const int t = c.token[lo] + 64 * (b - c.block[lo]);
-  seq_start[b] = c.block[lo];
-  tokens_of[b] = make_int2(t, min(64, c.token[lo + 1] - t));
+  const int s = c.sequence_of(b);
+  seq_start[b] = c.block[s];
+  tokens_of[b] = c.tokens_of(s, b);
 }
 
 struct PromptShape {
@@ -1626,27 +1648,39 @@ extern "C" int sale_prompt_attn(const sale_params_t* p, const void* q, const voi
   const int n_seqs = p->n_seqs > 0 ? p->n_seqs : 1;
   const int whole[2] = {0, p->seq_len};
   const int32_t* offsets = p->n_seqs > 0 ? p->cu_seqlens : whole;
-  int block = 0;
-  for (int s0 = 0; s0 < n_seqs; s0 += kTokenChunk) {
-    TokenChunk c;
-    c.n = min(kTokenChunk, n_seqs - s0);
-    const int first = block;
-    for (int e = 0; e <= c.n; ++e) {
-      if (e > 0) block += (offsets[s0 + e] - offsets[s0 + e - 1] + kBlockQ - 1) / kBlockQ;
-      c.block[e] = block;
-      c.token[e] = offsets[s0 + e];
-    }
-    if (block == first) continue;      // (sequences of no tokens)
-    token_table_kernel<<<dim3((unsigned)((block - first + 255) / 256)), dim3(256), 0, st>>>(c, w.seq_start, w.tokens_of);
-    if (hipGetLastError() != hipSuccess) return SALE_ERR_HIP;
-  }
   const long n_units = (long)g.n_qh * g.n_qb;
-  bool halves = two_waves_per_row({n_units, shape.even_rows, shape.longest, g.n_kvh, g.group, true, false, false, false, p->n_seqs > 0});
+  const bool halves = two_waves_per_row({n_units, shape.even_rows, shape.longest, g.n_kvh, g.group, true, false, false, false, p->n_seqs > 0});
   const bool sort = halves && shape.long_rows_wait;
-  const OrderJob job = {sort ? g.n_kvh : 0, nullptr, nullptr, w.order};
-  rearrange_kv_kernel<true, true, true><<<dim3((unsigned)(job.heads + g.n_kvh * g.n_qb)), dim3(256), 0, st>>>(
-      g, job, NoPass8{}, (const uint16_t*)k, (const uint16_t*)v, w.kp, w.vp, nullptr);
-  if (hipGetLastError() != hipSuccess) return SALE_ERR_HIP;
+  // f(chunk, its blocks, whether it is the last one): the sequences, as many at a time as travel with a launch
+  auto for_chunks = [&](auto f) -> int {
+    int block = 0;
+    for (int s0 = 0; s0 < n_seqs; s0 += kTokenChunk) {
+      TokenChunk c;
+      c.n = min(kTokenChunk, n_seqs - s0);
+      const int first = block;
+      for (int e = 0; e <= c.n; ++e) {
+        if (e > 0) block += (offsets[s0 + e] - offsets[s0 + e - 1] + kBlockQ - 1) / kBlockQ;
+        c.block[e] = block;
+        c.token[e] = offsets[s0 + e];
+      }
+      if (block == first) continue;      // (sequences of no tokens)
+      f(c, block - first, block == g.n_qb);
+      if (hipGetLastError() != hipSuccess) return SALE_ERR_HIP;
+    }
+    return SALE_OK;
+  };
+  if (sort) {
+    rc = for_chunks([&](const TokenChunk& c, int blocks, bool) {
+      token_table_kernel<<<dim3((unsigned)((blocks + 255) / 256)), dim3(256), 0, st>>>(c, w.seq_start, w.tokens_of);
+    });
+    if (rc != SALE_OK) return rc;
+  }
+  rc = for_chunks([&](const TokenChunk& c, int blocks, bool last) {
+    const OrderJob job = {sort && last ? g.n_kvh : 0, nullptr, nullptr, w.order};
+    rearrange_kv_kernel<true, true, true><<<dim3((unsigned)(job.heads + g.n_kvh * blocks)), dim3(256), 0, st>>>(
+        g, job, NoPass8{}, (const uint16_t*)k, (const uint16_t*)v, w.kp, w.vp, nullptr, c);
+  });
+  if (rc != SALE_OK) return rc;
   const int units = g.n_qb * g.group;
   const Qk8 none = {nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
   const RowFilter all = {nullptr, -1, 0, -1, 0, 0};

@@ -79,6 +79,20 @@ def test_a_sequence_does_not_depend_on_its_place(sale, n, hq, hkv):
         check(alone[0, h, some], None, want)
 
 
+def test_rows_sorted_by_length(sale):
+    """More sequences than travel with one launch, few enough rows that they are sorted: as in calls of a few of them."""
+    gen = torch.Generator().manual_seed(14)
+    new = [int(x) for x in torch.randint(193, 257, (300,), generator=gen)]
+    offsets = [int(x) for x in np.concatenate([[0], np.cumsum(new)])]
+    q, k, v = (rows((1, 1, offsets[-1], 128), "bhnd", gen) for _ in range(3))
+    o, lse = sale.prompt_attn(sale.Params(1, 1, 1, offsets[-1], cu_seqlens=tuple(offsets)), q, k, v, want_lse=True)
+    for a in range(0, 300, 60):
+        t0, t1 = offsets[a], offsets[a + 60]
+        p = sale.Params(1, 1, 1, t1 - t0, cu_seqlens=tuple(x - t0 for x in offsets[a:a + 61]))
+        part, part_lse = sale.prompt_attn(p, q[:, :, t0:t1], k[:, :, t0:t1], v[:, :, t0:t1], want_lse=True)
+        assert torch.equal(o[:, :, t0:t1], part) and torch.equal(lse[:, :, t0:t1], part_lse)
+
+
 @pytest.mark.parametrize("hq,hkv,n", [(2, 1, 75), (4, 4, 200)])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
 def test_a_later_token_that_is_not_finite(sale, hq, hkv, n, value):
