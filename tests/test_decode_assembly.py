@@ -1,0 +1,77 @@
+"""What decode.hip has to be compiled to, read from the assembly that the compiler makes of it.
+
+- No kernel keeps anything in scratch memory.  (With matrix results in ordinary registers this compiler has made wrong code of a
+  kernel that used accumulation registers and spilled.)
+- The pipeline's second product is inline assembly, which the compiler does not take for a matrix instruction: it inserts no waits.
+  Between what writes an operand of it and the product there have to be 2 wait states, between the product and anything but
+  another product that touches its result 18 (the longest that a product of 16 x 16 asks for)."""
+import os
+import re
+import subprocess
+
+import pytest
+
+from paper_2505_24179_amd import build
+
+
+@pytest.fixture(scope="module")
+def kernels(tmp_path_factory):
+    out = str(tmp_path_factory.mktemp("asm") / "decode.s")
+    r = subprocess.run([build.HIPCC, *build.FLAGS, "--offload-device-only", "-S", os.path.join(build.CSRC, "decode.hip"), "-o", out],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
+    text = open(out).read()
+    names = re.findall(r"^\s+\.name:\s+(_ZN4sale\S*kernel\S*)$", text, re.M)
+    scratch = re.findall(r"^\s+\.private_segment_fixed_size:\s+(\d+)$", text, re.M)
+    bodies = {n: text.split(f"\n{n}:", 1)[1].split("\n.Lfunc_end", 1)[0].splitlines() for n in names}
+    return dict(zip(names, map(int, scratch))), bodies
+
+
+def test_nothing_is_spilled(kernels):
+    scratch, _ = kernels
+    assert len(scratch) >= 16
+    assert not {n: b for n, b in scratch.items() if b}
+
+
+def _registers(text, kind):
+    found = {int(n) for n in re.findall(rf"\b{kind}(\d+)\b", text)}
+    for a, z in re.findall(rf"\b{kind}\[(\d+):(\d+)\]", text):
+        found |= set(range(int(a), int(z) + 1))
+    return found
+
+
+def test_inline_products_have_their_waits(kernels):
+    checked = 0
+    for name, body in kernels[1].items():
+        at, inline = 0, False
+        result, written = {}, {}      # wait state at which an inline product wrote, and another vector instruction
+        for line in body:
+            if "#ASMSTART" in line:
+                inline = True
+            elif "#ASMEND" in line:
+                inline = False
+            code = line.split(";")[0].strip()
+            if not code or code.startswith(".") or code.endswith(":"):
+                continue
+            op, _, rest = code.partition(" ")
+            args = [x.strip() for x in rest.split(",")]
+            at += 1 + (int(args[0]) if op == "s_nop" else 0)
+            if op.startswith("v_mfma") and inline:
+                checked += 1
+                sources = [("v", r) for r in _registers(",".join(args[1:3]), "v")] + [("a", r) for r in _registers(args[0], "a")]
+                near = [r for r in sources if at - written.get(r, -99) - 1 < 2]
+                assert not near, f"{name}: {code}: {near} written too shortly before"
+                for r in _registers(args[0], "a"):
+                    result[r] = at
+                    written.pop(("a", r), None)
+                continue
+            touched = _registers(rest, "a")
+            near = [r for r in touched if at - result.get(r, -99) - 1 < 18]
+            assert not near, f"{name}: {code}: {near} too shortly after an inline product"
+            if op.startswith("v_"):
+                for kind in "va":
+                    for r in _registers(args[0], kind):
+                        written[kind, r] = at
+                        if kind == "a":
+                            result.pop(r, None)
+    assert checked == 2 * 2 * 96      # bf16 and 8-bit pages, steps in one page or two, the products of two phases and the last ones
