@@ -49,6 +49,62 @@ def test_many_parts_and_many_rows(sale, batch, longest, prefix_len, kind):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("n", [5, 12])
+@pytest.mark.parametrize("page", [16, 128])
+def test_more_rows_than_a_tile_and_long_sequences(sale, kind, n, page):
+    gen = torch.Generator().manual_seed(n + page)
+    cache, prefix = make_cache(sale, [3000, 7, 1100, 0, 2049], 1, page, kind, "bnhd", gen, 0)
+    q = rows((5, 4, n, 128), "bnhd", gen, 2.0)
+    o, lse = sale.decode_attn(sale.Params(5, 4, 1, n), cache, q, want_lse=True)
+    check(o, lse, decode_oracle(cache, q, None, 0))
+
+
+def _some(sale, cache, q, o, lse, prefix, prefix_len, some):
+    part = sale.Cache(cache.k, cache.v, cache.table[some].contiguous(), cache.lens[some].contiguous(), cache.k_scale, cache.v_scale)
+    check(o[some], lse[some], decode_oracle(part, q[some], prefix, prefix_len))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("page,layout", [(16, "bhnd"), (32, "bnhd"), (64, "padded")])
+@pytest.mark.parametrize("batch,n,prefix_len", [(9, 2, 12000), (40, 1, 7001), (33, 3, 4133)])
+def test_many_rows_and_a_long_prefix(sale, kind, page, layout, batch, n, prefix_len):
+    """64 rows and more against many steps of the prefix, of whole pages and of what is left."""
+    gen = torch.Generator().manual_seed(batch + page)
+    cache, prefix = make_cache(sale, [3 + s % 5 for s in range(batch)], 1, page, kind, layout, gen, prefix_len)
+    q = rows((batch, 4, n, 128), layout, gen, 2.0)
+    o, lse = sale.decode_attn(sale.Params(batch, 4, 1, n), cache, q, prefix=prefix, prefix_len=prefix_len, want_lse=True)
+    _some(sale, cache, q, o, lse, prefix, prefix_len, [0, batch // 2, batch - 1])
+    again, _ = sale.decode_attn(sale.Params(batch, 4, 1, n), cache, q, prefix=prefix, prefix_len=prefix_len)
+    assert torch.equal(bits(again), bits(o))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("how", ["rising", "falling", "late", "huge", "missing"])
+def test_scores_of_a_long_prefix(sale, kind, page, how):
+    """Maxima that rise in every step, or in the first or last ones alone; scores of some ten thousands; pages that are none."""
+    gen = torch.Generator().manual_seed(page)
+    batch, prefix_len = 40, 5000
+    cache, prefix = make_cache(sale, [4] * batch, 1, page, kind, "bhnd", gen, prefix_len, spoil=False)
+    n_prefix = len(prefix)
+    ramp = {"rising": torch.linspace(0.01, 4, n_prefix), "falling": torch.linspace(4, 0.01, n_prefix), "late": torch.cat([torch.full((n_prefix - 1,), 0.01), torch.ones(1) * 4]),
+            "huge": torch.linspace(1, 60, n_prefix), "missing": torch.ones(n_prefix)}[how].cuda()
+    at = prefix.long()
+    if kind == "bf16":
+        cache.k[at] = (cache.k[at].float() * ramp[:, None, None, None]).bfloat16()
+    else:
+        codes = (cache.k.float() * 0.1)
+        codes[at] *= ramp[:, None, None, None]
+        cache.k.copy_(codes.clamp(-448, 448).to(torch.float8_e4m3fn))
+        cache.k_scale.mul_(10.0)
+    if how == "missing":
+        prefix[n_prefix // 2], prefix[n_prefix - 1], prefix[3] = -1, cache.k.shape[0], 2 ** 31 - 1
+    q = rows((batch, 4, 1, 128), "bhnd", gen, 3.0)
+    o, lse = sale.decode_attn(sale.Params(batch, 4, 1, 1), cache, q, prefix=prefix, prefix_len=prefix_len, want_lse=True)
+    _some(sale, cache, q, o, lse, prefix, prefix_len, [0, 17, batch - 1])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
 def test_pages_that_are_none_and_lens_that_lie(sale, kind):
     gen = torch.Generator().manual_seed(7)
     cache, prefix = make_cache(sale, [100, 100, 100, 64, 40, 70], 2, 16, kind, "bhnd", gen, 50, room=0, spoil=False)
