@@ -414,16 +414,18 @@ int sale_cache_copy(const sale_params_t* p, const sale_cache_t* cache, const int
  * Attention of the last seq_len tokens of every sequence (one when generating, more when drafted tokens are checked) to the
  * cache.  All sequences share a prefix of prefix_len keys, whose pages are prefix_table and which are read once for all
  * of them; a sequence's own keys, its new tokens among them (append first), follow it.  Query t of sequence s sees the
- * prefix and the own positions 0 .. lens[s] - seq_len + t.  O = softmax(Q K^T / sqrt(d)) V over these, probabilities
- * rounded to bf16 before the product with V and summed in fp32 before rounding.  A query that sees no key (an empty slot of
- * the batch) gets O = 0 and lse = -inf.  Keys that a query does not see have no effect, whatever is in their place.
+ * prefix and the own positions 0 .. lens[s] - seq_len + t.  O = softmax(Q K^T / sqrt(d)) V over these: sums of the
+ * probabilities in fp32; the factors of V are the probabilities rounded to bf16, or better.  A query that sees no key (an
+ * empty slot of the batch) gets O = 0 and lse = -inf.  Keys that a query does not see have no effect, whatever is in their
+ * place.
  *   p            : batch = sequences; n_q_heads / n_kv_heads * seq_len at most 64; n_seqs = 0
  *   q        in  : bf16, strided;  o out: bf16, strided
  *   prefix_table in : int32 [ceil(prefix_len / page_tokens)] (device), entries as in the table; NULL if prefix_len = 0
  *   lse      out : optional fp32 [batch][n_q_heads][seq_len], natural log of the sum
  *   ws           : workspace of sale_decode_workspace_bytes(p, cache, prefix_len) bytes (0: none needed)
- * How the keys are split over workgroups follows from the sizes given here, not from lens, so a captured call serves every
- * lens; results do not depend on what else runs.
+ * The workspace and the launches follow from the sizes given here, not from lens: a captured call serves every lens.  Which
+ * workgroup has which keys follows from all lens, so the last bits of a sequence's results may depend on the lengths of the
+ * others; the same arguments give the same bits.
  */
 int sale_decode_attn(const sale_params_t* p, const sale_cache_t* cache, const void* q,
                      const int32_t* prefix_table, int32_t prefix_len,

@@ -784,13 +784,20 @@ __global__ __launch_bounds__(512 * HALVES) void join_kernel(DecodeArgs a, int pr
   }
 }
 
-// How a call is cut, from its sizes alone.
-// kShares: workgroups that a call's own keys, and the parts of its prefix, are dealt to: two per CU.  64 sequences of 0 .. 8000
-// keys, page by page: 205.8 us with 256, 207.4 with 512, 208.1 with 1024, 210.9 with 2048, 217.8 with 4096; 4 sequences of 65000 ..
-// 131072 keys: 266.8, 263.6, 268.9, 275.7, 291.9.  (More of them only read and write more partial results.  Cut into a number of
-// parts that each sequence had to itself, the first took 251 us: the longest sequences' parts ended last.)
-constexpr int kShares = 512;
-constexpr int kWholeTurns = 6;
+// How a call is cut, as far as its sizes say (which share has which keys follows from lens).
+//
+// Workgroups for the own keys: one per CU reads as fast as more of them, which only make more partial results.  bf16, us with
+// 256, 512, 1024, 2048 workgroups: 64 sequences of 0 .. 8000 keys 198, 202, 202, 205; 4 of 65000 .. 131072 261, 265, 269, 275; one
+// of 32000 31.0, 35.2, 40.9; 16 of 500 .. 1000 19.9, 19.0, 20.2; 128 of 1000 .. 2000 150, 150, 160.  8-bit pages have half the bytes
+// in flight per workgroup and want two per CU where there is much to read: 128 of 1000 .. 2000 93.9, 83.0, 98.3; 16 of 4000 .. 8000
+// 47.5, 43.5, 47.3; but one of 8000 15.1, 18.3; one of 32000 23.6, 26.3.
+// The parts of the prefix likewise, of either type: 4 sequences behind 32000 keys 37.9, 42.2, 49.4, on 8-bit pages 28.0, 31.7, 38.1.
+// (Cut into a number of parts that each sequence had to itself, the 64 took 251: the parts of the longest ended last.)
+constexpr int kCus = 256, kPlentyTurns = 2048;
+// Without a prefix, short sequences are left whole: one launch, and nothing to join.  us, cut -> whole, 8 KV heads: one sequence of
+// 531 keys 14.9 -> 11.0, 750 15.0 -> 12.7, 1000 14.8 -> 15.5; 16 x 531 16.7 -> 12.5; 32 x 0 .. 1000 22.8 -> 18.9, 0 .. 1300 24.8 ->
+// 22.6; 128 x 0 .. 1300 75.6 -> 72.9.
+constexpr int kWholeTurns = 6, kManyUnits = 256, kWholeTurnsOfMany = 10;
 struct Plan {
   int own_tiles, pre_tiles;      // 16-row tiles per workgroup
   int shares, prefix_parts, prefix_chunk, row_tiles;
@@ -807,15 +814,17 @@ Plan make_plan(const sale_params_t* p, const sale_cache_t* c, int prefix_len) {
   auto up = [](long long a, long long b) { return (a + b - 1) / b; };
   auto clamp = [](long long x, long long lo, long long hi) { return (int)(x < lo ? lo : x > hi ? hi : x); };
   w.own_tiles = tiles_for(n_rows);
-  const long long turns = up((long long)c->table_width * c->page_tokens, kTurn) * p->batch;      // at most
-  w.whole = prefix_len == 0 && (long long)c->table_width * c->page_tokens <= kWholeTurns * kTurn;
-  w.shares = w.whole ? p->batch : clamp(up(kShares, p->n_kv_heads), 1, turns);
+  const long long units = (long long)p->batch * p->n_kv_heads;
+  const long long each = up((long long)c->table_width * c->page_tokens, kTurn), turns = each * p->batch;      // at most
+  w.whole = prefix_len == 0 && each <= (units >= kManyUnits ? kWholeTurnsOfMany : kWholeTurns);
+  const int workgroups = c->dtype == SALE_PAGE_FP8 && turns * p->n_kv_heads > kPlentyTurns ? 2 * kCus : kCus;
+  w.shares = w.whole ? p->batch : clamp(up(workgroups, p->n_kv_heads), 1, turns);
   if (w.whole) return w;
   if (prefix_len > 0) {
     w.pre_tiles = tiles_for(all_rows);
     w.row_tiles = (int)up(all_rows, 16 * w.pre_tiles);
     const long long groups = w.row_tiles * (long long)p->n_kv_heads;
-    const int parts = clamp(up(w.pre_tiles == 4 ? kShares / 2 : kShares, groups), 1,      // (64 rows: one workgroup per CU)
+    const int parts = clamp(up(kCus, groups), 1,
                             up(prefix_len, kTurn) < 128 ? up(prefix_len, kTurn) : 128);
     const int whole = w.pre_tiles == 4 ? 2 * kTurn : kTurn;      // (the pipeline takes steps by two)
     w.prefix_chunk = (int)(up(up(prefix_len, parts), whole) * whole);
@@ -866,7 +875,8 @@ void launch_decode(const DecodeArgs& a, const Plan& w, hipStream_t st) {
   const int n_rows = a.group * a.n_new, tiles = (n_rows + 15) / 16;
   const dim3 join((unsigned)((size_t)a.n_seqs * a.n_kvh * tiles));
   const int pre_rows = 16 * (w.pre_tiles > 0 ? w.pre_tiles : 1);
-  if (join.x > kShares) join_kernel<1><<<join, dim3(512), 0, st>>>(a, pre_rows);      // (more of them than fit at a time: small ones)
+  // (more of the large ones than fit at a time: 1024 of them, 128 sequences, 16.4 us, of the small ones 10.4)
+  if (join.x > 2 * kCus) join_kernel<1><<<join, dim3(512), 0, st>>>(a, pre_rows);
   else join_kernel<2><<<join, dim3(1024), 0, st>>>(a, pre_rows);
 }
 

@@ -140,7 +140,8 @@ class Cache:
     k_scale, v_scale fp32 [KV heads], 8-bit pages only: a key is value * k_scale
 
     Forking a sequence is copying its row of `table` and `lens` and, if its last page is partly filled, that page
-    (`cache_copy`) to a fresh one; freeing is handing its pages to others; compacting is `cache_copy` and new numbers in `table`."""
+    (`cache_copy`) to a fresh one; freeing is handing its pages to others; compacting is `cache_copy` and new numbers in `table`.
+    Contents may change between calls, shapes and strides may not (a new Cache takes others)."""
     k: torch.Tensor
     v: torch.Tensor
     table: torch.Tensor
