@@ -179,7 +179,7 @@ class Cache:
         for name, t in (("k_stride", self.k), ("v_stride", self.v)):
             if not t.is_contiguous():
                 getattr(c, name)[:] = t.stride()[:3]
-        return c, self.k.shape[1], self.k.shape[3], self.table.shape[0], self.k.get_device(), (self.k.shape[2], self.table.shape[1])
+        return c, self.k.shape[1], self.k.shape[3], self.table.shape[0], self.k.get_device(), (self.k.dtype, self.k.shape[2], self.table.shape[1])
 
     def _arg(self, p: "Params", sequences=None):
         """The C struct for a call with parameters p (over so many sequences)."""

@@ -110,3 +110,20 @@ def test_a_program(sale, page):
     for pool in pools:
         pool[len(used):] = float("nan")
     step(1)
+
+
+def test_caches_of_both_types_under_the_same_parameters(sale):
+    """Sizes that are kept with the parameters are kept by the type of the pages, whose workspaces differ where there is much to read."""
+    gen = torch.Generator().manual_seed(3)
+    p, q = sale.Params(4, 8, 8, 1), rows((4, 8, 1, 128), "bhnd", gen)
+    scale = torch.full((8,), 0.01, device="cuda")
+    pages = torch.randn(40, 8, 16, 128, generator=gen).cuda()
+    table = torch.full((4, 1024), -1, dtype=torch.int32)
+    table[:, :10] = torch.arange(40, dtype=torch.int32).view(4, 10)
+    table, lens = table.cuda(), torch.tensor([160, 3, 0, 77], dtype=torch.int32, device="cuda")
+    bf16 = sale.Cache(pages.bfloat16(), pages.bfloat16(), table, lens)
+    e4m3 = sale.Cache(*((pages / 0.01).clamp(-448, 448).to(torch.float8_e4m3fn) for _ in range(2)), table, lens, scale, scale)
+    alone = [sale.decode_attn(sale.Params(4, 8, 8, 1), c, q)[0] for c in (bf16, e4m3)]
+    assert sale.decode_workspace_bytes(p, bf16) != sale.decode_workspace_bytes(p, e4m3)
+    for c, want in zip((bf16, e4m3), alone):
+        assert torch.equal(sale.decode_attn(p, c, q)[0], want)
