@@ -157,8 +157,9 @@ class Cache:
                 raise ValueError(f"{name}: expected pages of torch.bfloat16 or torch.float8_e4m3fn, K and V alike, got {t.dtype}")
             if t.dim() != 4 or t.shape != self.k.shape or t.numel() == 0:
                 raise ValueError(f"{name}: expected [pages, KV heads, tokens, head_dim], K and V alike, got {tuple(t.shape)}")
-            if t.stride(3) != 1:
-                raise ValueError(f"{name}: the last dimension has to be contiguous, got strides {t.stride()}")
+            if t.stride(3) != 1 or t.stride(2) < t.shape[3]:
+                raise ValueError(f"{name}: the last dimension has to be contiguous and tokens at least head_dim apart, got strides "
+                                 f"{t.stride()}")
         if self.table.dim() != 2:
             raise ValueError(f"table: expected [sequences, pages], got {tuple(self.table.shape)}")
         _expect("table", self.table, torch.int32, self.table.numel())
@@ -180,6 +181,9 @@ class Cache:
             if not t.is_contiguous():
                 getattr(c, name)[:] = t.stride()[:3]
         return c, self.k.shape[1], self.k.shape[3], self.table.shape[0], self.k.get_device(), (self.k.dtype, self.k.shape[2], self.table.shape[1])
+
+    def __reduce__(self):      # (as that of Params)
+        return type(self), tuple(getattr(self, f.name) for f in fields(self))
 
     def _arg(self, p: "Params", sequences=None):
         """The C struct for a call with parameters p (over so many sequences)."""

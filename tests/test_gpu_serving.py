@@ -1,5 +1,7 @@
 """The serving calls as a program runs them: prompts of odd lengths, their keys and values into pages, a fork, a compaction, and
 tokens one by one and drafted, against one causal attention over everything that each sequence holds by then."""
+import copy
+
 import numpy as np
 import pytest
 import torch
@@ -127,3 +129,22 @@ def test_caches_of_both_types_under_the_same_parameters(sale):
     assert sale.decode_workspace_bytes(p, bf16) != sale.decode_workspace_bytes(p, e4m3)
     for c, want in zip((bf16, e4m3), alone):
         assert torch.equal(sale.decode_attn(p, c, q)[0], want)
+
+
+def test_copies_of_a_cache(sale):
+    """A deep copy, made after calls, has pages, table and lens of its own; and pages whose tokens overlap are refused."""
+    gen = torch.Generator().manual_seed(4)
+    p = sale.Params(2, 4, 2, 1)
+    pages = torch.randn(2, 4, 2, 16, 128, generator=gen).bfloat16().cuda()
+    table = torch.tensor([[2, 0], [1, 3]], dtype=torch.int32, device="cuda")
+    cache = sale.Cache(pages[0], pages[1], table, torch.tensor([20, 11], dtype=torch.int32, device="cuda"))
+    q, new = rows((2, 4, 1, 128), "bhnd", gen), rows((2, 2, 1, 128), "bhnd", gen)
+    before, _ = sale.decode_attn(p, cache, q)
+    other = copy.deepcopy(cache)
+    other.lens.add_(1)
+    sale.cache_append(p, other, new, new)
+    after, _ = sale.decode_attn(p, other, q)
+    assert torch.equal(sale.decode_attn(p, cache, q)[0], before) and not torch.equal(after, before)
+    flat = torch.zeros(128, dtype=torch.bfloat16, device="cuda").expand(1, 1, 16, 128)
+    with pytest.raises(ValueError, match="apart"):
+        sale.Cache(flat, flat, table, cache.lens)
