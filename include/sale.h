@@ -346,7 +346,8 @@ int sale_calibrate_tau(const sale_params_t* p, const void* q, const void* k, con
  * The calls below read batch, n_q_heads, n_kv_heads, seq_len, head_dim (128), the strides, n_seqs and cu_seqlens of
  * sale_params_t; its blocks (block_q .. local_blocks) are not read and flags must be 0.  seq_len is ANY positive number
  * here, and so are the lengths of packed sequences (n_seqs > 0: batch = 1; ascending offsets, two of which may be equal: a
- * sequence of no tokens).  Q, K, V, O and pages are 16-byte aligned (SALE_ERR_BAD_SHAPE).
+ * sequence of no tokens).  Q, K, V, O and pages are 16-byte aligned (SALE_ERR_BAD_SHAPE).  Sizes beyond what a launch or the
+ * kernels' 32-bit counts hold (2^24 row blocks of 64 tokens times heads, say) are refused (SALE_ERR_UNSUPPORTED).
  */
 
 /*

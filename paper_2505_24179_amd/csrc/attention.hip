@@ -1576,7 +1576,7 @@ PromptShape prompt_shape(const sale_params_t* p) {
     work += (long long)n * (n + 1);
   });
   const long long heads = (long long)p->batch * p->n_q_heads;
-  s.even_rows = (long)(heads * work / (s.longest + 1));
+  s.even_rows = (long)((double)heads * work / (s.longest + 1));
   long long after = 0;
   if (p->n_seqs > 0)
     for_sequences_from_last(p, [&](int a, int z) {
@@ -1612,7 +1612,8 @@ int validate_prompt(const sale_params_t* p) {
   if (rc != SALE_OK) return rc;
   const PromptShape s = prompt_shape(p);
   if (s.longest > kMaxSeqLen / kBlockQ) return SALE_ERR_UNSUPPORTED;
-  if (s.blocks * p->batch * p->n_q_heads > 0x3FFFFFFFLL || s.blocks > 0x1FFFFFFLL) return SALE_ERR_UNSUPPORTED;      // (32-bit indices)
+  const long long heads = (long long)p->batch * p->n_q_heads;
+  if (s.blocks > kMostWorkgroups || heads > kMostWorkgroups || s.blocks * heads > kMostWorkgroups) return SALE_ERR_UNSUPPORTED;
   return SALE_OK;
 }
 

@@ -233,9 +233,11 @@ extern "C" int sale_cache_append(const sale_params_t* p, const sale_cache_t* cac
   a.n_kvh = p->n_kv_heads;
   a.heads_first = a.sk.sh < a.sk.st ? 1 : 0;
   a.tile = kAppendRows / p->n_kv_heads < 1 ? 1 : kAppendRows / p->n_kv_heads;
+  // (of packed sequences at most, in any of the launches)
+  const long long most = p->n_seqs > 0 ? (long long)p->seq_len / a.tile + kAppendChunk : ((long long)(p->seq_len - 1) / a.tile + 1) * p->batch;
+  if (most > kMostWorkgroups) return SALE_ERR_UNSUPPORTED;
   const hipStream_t st = (hipStream_t)stream;
   auto launch = [&](long long workgroups) -> int {
-    if (workgroups > 0x7FFFFFFF) return SALE_ERR_UNSUPPORTED;
     if (cache->dtype == SALE_PAGE_FP8) append_kernel<true><<<dim3((unsigned)workgroups), dim3(256), 0, st>>>(a);
     else append_kernel<false><<<dim3((unsigned)workgroups), dim3(256), 0, st>>>(a);
     return hipGetLastError() == hipSuccess ? SALE_OK : SALE_ERR_HIP;
@@ -279,7 +281,7 @@ extern "C" int sale_cache_copy(const sale_params_t* p, const sale_cache_t* cache
   const long long page_bytes = (long long)p->n_kv_heads * cache->page_tokens << (a.row_shift + 4);
   if (page_bytes > (1LL << 30)) return SALE_ERR_UNSUPPORTED;      // (pieces of a launch are counted in 32 bits)
   a.parts = (int)((page_bytes + kCopyBytes - 1) / kCopyBytes);
-  const int chunk = (int)min((long long)kCopyChunk, max(1LL, 0x7FFFFFFFLL / (2LL * a.parts)));
+  const int chunk = (int)min((long long)kCopyChunk, max(1LL, kMostWorkgroups / (2LL * a.parts)));
   for (int i0 = 0; i0 < n; i0 += chunk) {
     const int m = min(chunk, n - i0);
     for (int i = 0; i < m; ++i) { a.src[i] = src[i0 + i]; a.dst[i] = dst[i0 + i]; }

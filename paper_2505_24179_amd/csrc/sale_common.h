@@ -197,6 +197,7 @@ enum GeomClass { kGeomQuantize, kGeomPath };
 int validate_common(const sale_params_t* p, GeomClass cls);
 int validate_tokens(const sale_params_t* p);      // the serving calls: any length, no blocks, no flags
 Strided layout_of(const int64_t* stride, int heads, int seq_len);      // all-zero strides: contiguous
+constexpr long long kMostWorkgroups = 0xFFFFFF;      // of 256 threads: a launch has fewer than 2^32 threads
 size_t prompt_workspace_bytes(const sale_params_t* p);      // 0 if the parameters are invalid
 // attention launcher shared by the attention entry points and the calibration (attention.hip)
 int launch_attn_rows(const sale_params_t* p, const void* q, const void* k, const void* v, const uint64_t* mask,

@@ -107,6 +107,19 @@ def test_sizes_that_are_not_supported(sale):
     assert lib.sale_prompt_attn(b(_params(sale, batch=1 << 20, n=262144)), F, F, F, F, None, F, 1 << 60, None) == -3
 
 
+def test_launches_of_too_many_threads(sale):
+    """2^24 workgroups of 256 threads and more."""
+    lib, c, b = sale.raw(), _cache(sale), ctypes.byref
+    append = lambda p: lib.sale_cache_append(b(p), b(c), F, F, None)
+    assert append(_params(sale, batch=1, hq=32, hkv=32, n=1 << 24)) == -3      # a workgroup per token
+    assert append(_params(sale, batch=1 << 24, hq=32, hkv=32, n=1)) == -3
+    assert append(_params(sale, batch=1, hq=32, hkv=32, n=1 << 24, cu_seqlens=(0, 5, 1 << 24))) == -3
+    big = (1 << 31) - 1
+    for kw in (dict(batch=1 << 12, n=1 << 17), dict(batch=big, hq=big, hkv=big, n=64), dict(batch=big, hq=1, hkv=1, n=big)):
+        assert lib.sale_workspace_bytes(b(_params(sale, **kw)), sale.WS_PROMPT_ATTN) == 0
+        assert lib.sale_prompt_attn(b(_params(sale, **kw)), F, F, F, F, None, F, 1 << 60, None) == -3
+
+
 def test_workspaces(sale):
     lib, c, b = sale.raw(), _cache(sale), ctypes.byref
     p = _params(sale, n=100)
