@@ -16,6 +16,14 @@
 //   belongs to the same key, 16 t + 4 r + g, that it loads of V as number 4 t + r: the probabilities are the B operand as they
 //   are.  No LDS, no exchange between lanes in the loop.
 // The 4 waves of a workgroup take every fourth step of its keys and join at the end through LDS.
+//
+// What bounds it.  A sequence's own keys: HBM, each key is read once.  8 KV heads, 4 queries each: 64 sequences of 0 .. 8000
+// keys (1.05 GB) 191 us, 5.5 TB/s; 4 of 65000 .. 131072 (1.53 GB) 250 us, 6.1 TB/s, where a copy of 1 GB runs at 5.1; then 7 - 10 us
+// for the join.  One sequence of 531 keys: 11 us, latency from the launch to the last of four turns.
+// The prefix: the instructions of a wave.  128 sequences x 4 queries behind 32749 keys (8 KV heads, 69 GFLOP) 100 us, 690
+// TFLOP/s, and the prefix is fetched once for all rows (136 MB); 32 keys for 64 rows are 64 matrix instructions, 177 vector,
+// 67 - 90 scalar ones and 17 loads, 1.2 us; waves issue half of the time and wait for a pipe in another third.  It takes as long
+// with 8-bit pages, or when all pages are the same one; two such waves per SIMD with 32 rows each take 36 % longer.
 #include "cache.h"
 
 namespace sale {
