@@ -326,12 +326,19 @@ __device__ __forceinline__ void sweep(const CacheView& c, const Keys& ks, int kv
 //   S(t + 1) = K(t + 1) Q^T     MFMA
 //   O += V(t - 1)^T P(t - 1)^T  MFMA
 //   P(t) = exp2(S(t) - ref)     VALU, its sums, the turning of V(t - 1) and the largest of the scores S(t + 1)
-//   loads of K(t + 3), V(t + 1) into the registers that were just read
+//   K(t + 3) to LDS, K(t + 2) from there and V(t + 1) into the registers that were just read (8-bit: K(t + 3) too)
 // has no dependency between its streams; they are laid side by side by hand, an MFMA and its share of the rest at a time, for a
-// wave is alone on its SIMD (64 rows: 128 accumulators, 64 registers of Q, 64 of S, 128 of K and V).
+// wave is alone on its SIMD (64 rows: 128 accumulators, 64 registers of Q, 64 of S, 96 of K and V).
+//
+// K of bf16 goes through LDS, straight from memory and each wave's for itself: the operand of 16 lanes is 16 bytes of each of 16 keys,
+// and a load from memory that touches 16 lines for 16 lanes keeps the CU's one load path busy four times as long as one of whole
+// keys.  A load brings 1 KB of neighbouring keys; in LDS a key is a row, in which chunk c of 16 bytes lies at place c ^ m, m the row of
+// the operand that the key becomes.  (128 sequences behind 32749 keys: operands straight from memory 100 us, this way 83.  Keys of
+// 8 bits are half the loads, and conversions take the time: 31.2 straight, 31.9 this way.)
+struct KeyBuffer { u32x4 of[kWaves][512]; };      // the keys of a step of every wave
 template <bool FP8, bool ONE>
-__device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int kvh, int key0, int steps, int lane, float scale,
-                                         Rows<FP8, 4>& rows) {
+__device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int kvh, int key0, int steps, int lane, int wave, float scale,
+                                         KeyBuffer& even, KeyBuffer& odd, Rows<FP8, 4>& rows) {
   constexpr int NT = 4, kQk = 8 * NT, kPv = 8 * NT, kElems = 8 * NT, kLoads = FP8 ? 2 : 4;
   const int mask = (1 << c.page_shift) - 1;
   const LaneOffsets lane_at = lane_offsets<FP8>(c, lane);
@@ -352,8 +359,44 @@ __device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int
       return {slots_of(side, head, id.a, slot), slots_of(side, head, id.b, (slot + 16) & mask)};
     }
   };
-  Operands<FP8> x[2];      // [t % 2]
-  auto get_k = [&](Operands<FP8>& to, const Tiles& from, int t, int s) __attribute__((always_inline)) { load_k<FP8>(to, t, s, t == 0 ? from.a : from.b, lane_at.k); };
+  Operands<FP8> x[2];      // V: [t % 2]; K: 8-bit likewise, bf16 the next one that is needed, in x[0]
+  // bf16: a lane's offset in memory in load s of a 16-key tile, which brings keys 4 s .. 4 s + 3, and in LDS of operand s
+  int to_lane[4], from_lane[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    const int m = lane & 15, g = lane >> 4, key = 4 * s + g;      // (key 4 s + g becomes row s + 4 g)
+    to_lane[s] = key * (int)c.k.token + 16 * (m ^ (s + 4 * g));
+    from_lane[s] = (4 * (m & 3) + (m >> 2)) * 16 + ((4 * s + g) ^ m);
+  }
+  auto get_k = [&](auto parity, const Tiles& from, int t, int s) __attribute__((always_inline)) {
+    constexpr int p = decltype(parity)::value;
+    if constexpr (FP8) load_k<FP8>(x[p], t, s, t == 0 ? from.a : from.b, lane_at.k);
+    else __builtin_amdgcn_raw_ptr_buffer_load_lds(t == 0 ? from.a : from.b, (__attribute__((address_space(3))) void*)&(p ? odd : even).of[wave][256 * t + 64 * s],
+                                                  16, to_lane[s], 0, 0, 0);
+  };
+  auto read_k = [&](auto parity, int t, int s) __attribute__((always_inline)) {
+    if constexpr (!FP8) x[0].k[t][s] = (decltype(parity)::value ? odd : even).of[wave][256 * t + from_lane[s]];
+  };
+  constexpr std::integral_constant<int, 0> in_even{};
+  constexpr std::integral_constant<int, 1> in_odd{};
+  // What was read from LDS has arrived: its place can be written again.
+  auto arrived = [&]() __attribute__((always_inline)) {
+    if constexpr (FP8) return;
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xC07F);      // lgkmcnt(0)
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // All loads but the last `newer` have arrived.  (The compiler takes a load to LDS for a write of 16 bytes, where it writes 1 KB, and
+  // does not wait for all that a read from there needs.)
+  auto loaded = [&](auto newer) __attribute__((always_inline)) {
+    constexpr int n = decltype(newer)::value;
+    if constexpr (FP8) return;      // (registers: the compiler's waits)
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt((n & 15) | (n >> 4) << 14 | 0x0F70);      // vmcnt(n)
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  constexpr std::integral_constant<int, 8> k_newer{};       // newer than what is waited for: K of a step
+  constexpr std::integral_constant<int, 16> kv_newer{};     // .., and V of one
   auto get_v = [&](Operands<FP8>& to, const Tiles& from, int j) __attribute__((always_inline)) { load_v<FP8>(to, j, j < 4 ? from.a : from.b, lane_at.v, c.v.token); };
   // O += V P with the accumulators in AGPRs, where the compiler would move them back and forth: S, P and V take most of the 256
   // ordinary registers.  The compiler does not see a matrix instruction here, so its waits are this code's to keep: 2 states from
@@ -402,25 +445,34 @@ __device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int
     }
   };
   TwoPages id1 = ids_of(1), id2 = ids_of(2), id3 = ids_of(3);
-  auto get_all_k = [&](Operands<FP8>& to, int u, TwoPages id) __attribute__((always_inline)) {
+  auto get_all_k = [&](auto parity, int u, TwoPages id) __attribute__((always_inline)) {
     const Tiles from = tiles_of(c.k, k_head, u, id);
 #pragma unroll
-    for (int n = 0; n < 2 * kLoads; ++n) get_k(to, from, n / kLoads, n % kLoads);
+    for (int n = 0; n < 2 * kLoads; ++n) get_k(parity, from, n / kLoads, n % kLoads);
   };
-  {
-    const TwoPages id0 = ids_of(0);
-    get_all_k(x[0], 0, id0);
-    get_all_k(x[1], 1, id1);
-    const Tiles from = tiles_of(c.v, v_head, 0, id0);
+  auto read_all_k = [&](auto parity) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) get_v(x[0], from, j);
-  }
+    for (int n = 0; n < 8; ++n) read_k(parity, n / 4, n % 4);
+  };
+  const TwoPages id0 = ids_of(0);
+  get_all_k(in_even, 0, id0);
+  get_all_k(in_odd, 1, id1);
+  loaded(k_newer);
+  read_all_k(in_even);
 #pragma unroll
   for (int n = 0; n < kQk; ++n) {
     const int t = n / 16, s = n / 4 % 4, qt = n % 4;
     S[0][t][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand(x[0], t, s), rows.q[qt][s], s == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : S[0][t][qt], 0, 0, 0);
   }
-  get_all_k(x[0], 2, id2);
+  arrived();
+  get_all_k(in_even, 2, id2);
+  {
+    const Tiles from = tiles_of(c.v, v_head, 0, id0);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) get_v(x[0], from, j);
+  }
+  loaded(kv_newer);
+  read_all_k(in_odd);
 #pragma unroll
   for (int qt = 0; qt < NT; ++qt)
 #pragma unroll
@@ -430,6 +482,9 @@ __device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int
   raise(0, P[1]);
   auto phase = [&](auto xc, int t) __attribute__((always_inline)) {
     constexpr int cur = decltype(xc)::value, oth = 1 - cur;
+    constexpr std::integral_constant<int, cur> in_cur{};
+    constexpr std::integral_constant<int, oth> in_oth{};
+    arrived();
     const Tiles k_next = tiles_of(c.k, k_head, t + 3, id3), v_next = tiles_of(c.v, v_head, t + 1, id1);
     id1 = id2; id2 = id3; id3 = ids_of(t + 4);
     float E[kElems], top[NT];
@@ -460,15 +515,17 @@ __device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int
       constexpr int i = decltype(ic)::value;
       if constexpr (i < kQk) {
         constexpr int t2 = i / 16, s = i / 4 % 4, qt = i % 4;
-        if constexpr (qt == 0) k = k_operand(x[oth], t2, s);
+        if constexpr (qt == 0) k = k_operand(x[FP8 ? oth : 0], t2, s);
         S[oth][t2][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, rows.q[qt][s], s == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : S[oth][t2][qt], 0, 0, 0);
-        if constexpr (qt == 3 && !FP8) get_k(x[oth], k_next, t2, s);
-        if constexpr (qt == 3 && FP8 && s % 2 == 1) get_k(x[oth], k_next, t2, s / 2);
+        if constexpr (qt == 1 && !FP8) get_k(in_oth, k_next, t2, s);
+        if constexpr (qt == 1 && FP8 && s % 2 == 1) get_k(in_oth, k_next, t2, s / 2);
         if constexpr (i == kQk - 4) v[0] = turned<FP8>(x[oth], 0);
       } else {
         constexpr int e = (i - kQk) / 4, qt = i % 4;
         pv(std::false_type{}, qt, e, v[e % 2], P[oth][qt]);
         if constexpr (qt == 0 && e < 7) v[(e + 1) % 2] = turned<FP8>(x[oth], e + 1);
+        if constexpr (i == kQk) loaded(kv_newer);
+        if constexpr (qt == 1) read_k(in_cur, e / 4, e % 4);
         if constexpr (e >= 6) get_v(x[oth], v_next, 4 * (e - 6) + qt);
       }
       constexpr int from = i * slots / (kQk + kPv), to = (i + 1) * slots / (kQk + kPv);
@@ -492,6 +549,7 @@ __device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int
     for (int qt = 0; qt < NT; ++qt) pv(std::true_type{}, qt, e, v, P[1][qt]);
   }
   settle();
+  loaded(std::integral_constant<int, 0>{});      // (what was requested beyond the end arrives while the workgroup is there)
 }
 
 // The sum over the four lanes that are equal modulo 16.
@@ -690,8 +748,10 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void prefix_kernel(De
     for (int i = (lo >> a.c.page_shift) + lane; i <= (hi - 1) >> a.c.page_shift; i += 64) missing |= (unsigned)ks.table[i] >= (unsigned)a.c.n_pages;
     const int steps = (max(hi - from, 0) / kStep + kWaves - 1) / kWaves & ~1;
     if (steps > 0 && __builtin_amdgcn_ballot_w64(missing) == 0) {
-      if (a.c.page_shift >= 5) pipeline<FP8, true>(a.c, ks, kvh, from, steps, lane, scale, rows);
-      else pipeline<FP8, false>(a.c, ks, kvh, from, steps, lane, scale, rows);
+      // (Aligned so that they come first in LDS, below 64 KB: a load's place there is documented as a number of 16 bits.)
+      __shared__ __attribute__((aligned(1024))) KeyBuffer even, odd;
+      if (a.c.page_shift >= 5) pipeline<FP8, true>(a.c, ks, kvh, from, steps, lane, wave, scale, even, odd, rows);
+      else pipeline<FP8, false>(a.c, ks, kvh, from, steps, lane, wave, scale, even, odd, rows);
       from += steps * kTurn;
     }
   }

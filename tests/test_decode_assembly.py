@@ -75,3 +75,36 @@ def test_inline_products_have_their_waits(kernels):
                         if kind == "a":
                             result.pop(r, None)
     assert checked == 2 * 2 * 96      # bf16 and 8-bit pages, steps in one page or two, the products of two phases and the last ones
+
+
+def test_keys_in_lds_have_their_waits(kernels):
+    """The pipeline's keys go to LDS by loads that write there (L); the reads of them (R), which follow, need all of a step to have
+    arrived, and what comes next to a buffer, that its reads have.  w, W: at most 8, 16 of the loads (P: others) are outstanding.  K: no
+    read is."""
+    phases = prologues = 0
+    for name, body in kernels[1].items():
+        blocks = [[]]
+        for line in body:
+            if re.match(r"\.LBB\S+:", line) or line.lstrip().startswith("; %bb."):
+                blocks.append([])
+            blocks[-1].append(line.split(";")[0].strip())
+        for block in blocks:
+            events = ""
+            for code in block:
+                vm, lgkm = re.search(r"vmcnt\((\d+)\)", code), re.search(r"lgkmcnt\((\d+)\)", code)
+                if code.startswith("s_waitcnt"):
+                    events += "w" if vm and int(vm[1]) <= 8 else "W" if vm and int(vm[1]) <= 16 else ""
+                    events += "K" if lgkm and int(lgkm[1]) == 0 else ""
+                elif code.startswith(("buffer_load", "global_load")):
+                    events += "L" if code.endswith(" lds") else "P"
+                elif code.startswith("ds_read_b128"):
+                    events += "R"
+            if "L" not in events:
+                continue
+            if sum(code.startswith("v_mfma") for code in block) >= 60:
+                phases += 1
+                assert re.fullmatch(r"K+L{8}[wW]+[RP]{16}", events) and events.count("R") == 8, (name, events)
+            else:
+                prologues += 1
+                assert re.match(r"K*L{16}w+(?:RK*){8}(?<=K)L{8}P{8}[wW]+(?:RK*){8}", events), (name, events)
+    assert (phases, prologues) == (4, 2)
