@@ -858,10 +858,13 @@ __global__ __launch_bounds__(512 * HALVES) void join_kernel(DecodeArgs a, int pr
 // 256, 512, 1024, 2048 workgroups: 64 sequences of 0 .. 8000 keys 198, 202, 202, 205; 4 of 65000 .. 131072 261, 265, 269, 275; one
 // of 32000 31.0, 35.2, 40.9; 16 of 500 .. 1000 19.9, 19.0, 20.2; 128 of 1000 .. 2000 150, 150, 160.  8-bit pages have half the bytes
 // in flight per workgroup and want two per CU where there is much to read: 128 of 1000 .. 2000 93.9, 83.0, 98.3; 16 of 4000 .. 8000
-// 47.5, 43.5, 47.3; but one of 8000 15.1, 18.3; one of 32000 23.6, 26.3.
+// 47.5, 43.5, 47.3; but one of 8000 15.1, 18.3; one of 32000 23.6, 26.3.  So do short sequences (here behind a prefix), whose pieces
+// each begin with a wait that another workgroup can fill: kernel, 256, 512, 768 workgroups, 128 of 0 .. 300 keys 24.1, 17.6, 19.9;
+// 0 .. 1000 48.4, 44.8, 44.1, four new tokens each 54.6, 47.1, 46.2; 32 of 0 .. 1000 17.5, 15.6, 15.1; but 0 .. 2000 101, 102, 102, and 0 .. 4000
+// 188, 193, 189.
 // The parts of the prefix likewise, of either type: 4 sequences behind 32000 keys 37.9, 42.2, 49.4, on 8-bit pages 28.0, 31.7, 38.1.
 // (Cut into a number of parts that each sequence had to itself, the 64 took 251: the parts of the longest ended last.)
-constexpr int kCus = 256, kPlentyTurns = 2048;
+constexpr int kCus = 256, kPlentyTurns = 2048, kShortTurns = 12;
 // Without a prefix, short sequences are left whole: one launch, and nothing to join.  us, cut -> whole, 8 KV heads: one sequence of
 // 531 keys 14.9 -> 11.0, 750 15.0 -> 12.7, 1000 14.8 -> 15.5; 16 x 531 16.7 -> 12.5; 32 x 0 .. 1000 22.8 -> 18.9, 0 .. 1300 24.8 ->
 // 22.6; 128 x 0 .. 1300 75.6 -> 72.9.
@@ -885,7 +888,8 @@ Plan make_plan(const sale_params_t* p, const sale_cache_t* c, int prefix_len) {
   const long long units = (long long)p->batch * p->n_kv_heads;
   const long long each = up((long long)c->table_width * c->page_tokens, kTurn), turns = each * p->batch;      // at most
   w.whole = prefix_len == 0 && each <= (units >= kManyUnits ? kWholeTurnsOfMany : kWholeTurns);
-  const int workgroups = c->dtype == SALE_PAGE_FP8 && turns * p->n_kv_heads > kPlentyTurns ? 2 * kCus : kCus;
+  const bool two = each <= kShortTurns || (c->dtype == SALE_PAGE_FP8 && turns * p->n_kv_heads > kPlentyTurns);
+  const int workgroups = two ? 2 * kCus : kCus;
   w.shares = w.whole ? p->batch : clamp(up(workgroups, p->n_kv_heads), 1, turns);
   if (w.whole) return w;
   if (prefix_len > 0) {
