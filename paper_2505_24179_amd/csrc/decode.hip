@@ -117,13 +117,13 @@ __device__ __forceinline__ LaneOffsets lane_offsets(const CacheView& c, int lane
   return {(int)((4 * (m & 3) + (m >> 2)) * c.k.token) + 16 * g, (int)(g * c.v.token) + (FP8 ? 8 : 16) * m};
 }
 template <bool FP8>
-__device__ __forceinline__ void load_k(Operands<FP8>& x, int t, int s, __amdgpu_buffer_rsrc_t from, int lane_offset) {
-  x.k[t][s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, lane_offset + 64 * s, 0, 0));
+__device__ __forceinline__ void load_k(Operands<FP8>& x, int t, int s, __amdgpu_buffer_rsrc_t from, int lane_offset, int at = 0) {
+  x.k[t][s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, lane_offset + 64 * s, at, 0));
 }
 template <bool FP8>
-__device__ __forceinline__ void load_v(Operands<FP8>& x, int j, __amdgpu_buffer_rsrc_t from, int lane_offset, uint32_t token) {
-  if constexpr (FP8) x.v[j] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(from, lane_offset, 4 * (j & 3) * token, 0));
-  else x.v[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, lane_offset, 4 * (j & 3) * token, 0));
+__device__ __forceinline__ void load_v(Operands<FP8>& x, int j, __amdgpu_buffer_rsrc_t from, int lane_offset, int at) {
+  if constexpr (FP8) x.v[j] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(from, lane_offset, at, 0));
+  else x.v[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, lane_offset, at, 0));
 }
 
 template <bool FP8>
@@ -138,7 +138,7 @@ __device__ __forceinline__ void load_step(const CacheView& c, const Keys& ks, in
 #pragma unroll
     for (int s = 0; s < (FP8 ? 2 : 4); ++s) load_k<FP8>(x, t, s, k, at.k);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) load_v<FP8>(x, 4 * t + r, v, at.v, c.v.token);
+    for (int r = 0; r < 4; ++r) load_v<FP8>(x, 4 * t + r, v, at.v, 4 * r * c.v.token);
   }
 }
 
@@ -349,12 +349,14 @@ __device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int
     const int key = key_of(u), a = entry_at(ks.table, key >> c.page_shift);
     return {a, ONE ? a : entry_at(ks.table, (key + 16) >> c.page_shift)};
   };
-  struct Tiles { __amdgpu_buffer_rsrc_t a, b; };
+  struct Tiles { __amdgpu_buffer_rsrc_t a, b; };      // (the same where a step lies in a page)
+  const int k_second = ONE ? 16 * (int)c.k.token : 0, v_second = ONE ? 16 * (int)c.v.token : 0;      // offset of the second tile
   auto tiles_of = [&](const PageSide& side, const uint8_t* head, int u, TwoPages id) __attribute__((always_inline)) -> Tiles {
     const int slot = key_of(u) & mask;
     if constexpr (ONE) {
       const uint8_t* at = head + (uint64_t)(uint32_t)id.a * side.page + (uint32_t)slot * side.token;
-      return {operand_buffer(at, 0x7FFFFFF0), operand_buffer(at + 16 * side.token, 0x7FFFFFF0)};
+      const __amdgpu_buffer_rsrc_t both = operand_buffer(at, 0x7FFFFFF0);
+      return {both, both};
     } else {
       return {slots_of(side, head, id.a, slot), slots_of(side, head, id.b, (slot + 16) & mask)};
     }
@@ -370,9 +372,9 @@ __device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int
   }
   auto get_k = [&](auto parity, const Tiles& from, int t, int s) __attribute__((always_inline)) {
     constexpr int p = decltype(parity)::value;
-    if constexpr (FP8) load_k<FP8>(x[p], t, s, t == 0 ? from.a : from.b, lane_at.k);
+    if constexpr (FP8) load_k<FP8>(x[p], t, s, t == 0 ? from.a : from.b, lane_at.k, t * k_second);
     else __builtin_amdgcn_raw_ptr_buffer_load_lds(t == 0 ? from.a : from.b, (__attribute__((address_space(3))) void*)&(p ? odd : even).of[wave][256 * t + 64 * s],
-                                                  16, to_lane[s], 0, 0, 0);
+                                                  16, to_lane[s], t * k_second, 0, 0);
   };
   auto read_k = [&](auto parity, int t, int s) __attribute__((always_inline)) {
     if constexpr (!FP8) x[0].k[t][s] = (decltype(parity)::value ? odd : even).of[wave][256 * t + from_lane[s]];
@@ -397,7 +399,7 @@ __device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int
   };
   constexpr std::integral_constant<int, 8> k_newer{};       // newer than what is waited for: K of a step
   constexpr std::integral_constant<int, 16> kv_newer{};     // .., and V of one
-  auto get_v = [&](Operands<FP8>& to, const Tiles& from, int j) __attribute__((always_inline)) { load_v<FP8>(to, j, j < 4 ? from.a : from.b, lane_at.v, c.v.token); };
+  auto get_v = [&](Operands<FP8>& to, const Tiles& from, int j) __attribute__((always_inline)) { load_v<FP8>(to, j, j < 4 ? from.a : from.b, lane_at.v, 4 * (j & 3) * c.v.token + (j < 4 ? 0 : v_second)); };
   // O += V P with the accumulators in AGPRs, where the compiler would move them back and forth: S, P and V take most of the 256
   // ordinary registers.  The compiler does not see a matrix instruction here, so its waits are this code's to keep: 2 states from
   // what writes v, p or acc to the product (in a phase 3 other products are between, elsewhere s_nop 1), and from the product to
