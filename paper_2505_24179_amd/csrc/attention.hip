@@ -1543,8 +1543,8 @@ int launch_attn_rows(const sale_params_t* p, const void* q, const void* k, const
 // partly filled, follow each other; a table says which tokens a block holds.  K' and V' are made for whole blocks (V' zero
 // behind the last token), so the sweep itself is that of the dense kernel, instruction for instruction; only Q, O and lse
 // are addressed by token, and what is not finite in V is kept from queries before its key (key_by_key).
-// What bounds it is what bounds the dense sweep, the matrix unit: 32705 tokens of 32 / 8 heads (8.76 TFLOP) 6.80 ms, 1.29 PFLOP/s,
-// and 44 us for the copies; six sequences of 24433 tokens together (1.79 TFLOP) 1.5 ms and 37 us; where the library's product of
+// What bounds it is what bounds the dense sweep, the matrix unit: 32705 tokens of 32 / 8 heads (8.76 TFLOP) 6.8 - 7.0 ms, 1.25 - 1.29
+// PFLOP/s, and 44 us for the copies; six sequences of 24433 tokens together (1.79 TFLOP) 1.5 ms and 37 us; where the library's product of
 // two 8192 x 8192 matrices runs at 1.20 - 1.27.  Short ones: latency, six of 1 .. 333 tokens 5.5 + 13.9 us.
 namespace {
 

@@ -14,16 +14,17 @@
 //      8 m + c in row m.
 //   The key of a tile that K's row 4 g + r holds is 4 r + g, so the score that lane (n, g) gets in register r of tile t
 //   belongs to the same key, 16 t + 4 r + g, that it loads of V as number 4 t + r: the probabilities are the B operand as they
-//   are.  No LDS, no exchange between lanes in the loop.
+//   are.  No exchange between lanes in the loop.
 // The 4 waves of a workgroup take every fourth step of its keys and join at the end through LDS.
 //
 // What bounds it.  A sequence's own keys: HBM, each key is read once.  8 KV heads, 4 queries each: 64 sequences of 0 .. 8000
 // keys (1.05 GB) 191 us, 5.5 TB/s; 4 of 65000 .. 131072 (1.53 GB) 250 us, 6.1 TB/s, where a copy of 1 GB runs at 5.1; then 7 - 10 us
-// for the join.  One sequence of 531 keys: 11 us, latency from the launch to the last of four turns.
-// The prefix: the instructions of a wave.  128 sequences x 4 queries behind 32749 keys (8 KV heads, 69 GFLOP) 100 us, 690
-// TFLOP/s, and the prefix is fetched once for all rows (136 MB); 32 keys for 64 rows are 64 matrix instructions, 177 vector,
-// 67 - 90 scalar ones and 17 loads, 1.2 us; waves issue half of the time and wait for a pipe in another third.  It takes as long
-// with 8-bit pages, or when all pages are the same one; two such waves per SIMD with 32 rows each take 36 % longer.
+// for the join.  One sequence of 531 keys: 11 us, latency from the launch to the last of five turns.
+// The prefix: the instructions of a wave, and its loads beside them.  128 sequences x 4 queries behind 32749 keys (8 KV heads, 69
+// GFLOP) 83 us, 830 TFLOP/s, and the prefix is fetched once for all rows (136 MB).  32 keys for 64 rows are 64 matrix, 175 vector and 60
+// scalar instructions, 16 loads and 8 reads from LDS: 1.1 us, of which 0.8 are left without the loads and reads; 11 us are the launch, the
+// first loads and the join of the waves.  (8-bit pages: half the loads and 64 conversions more, 1.15 us.)  Two such waves per SIMD with 32
+// rows each took 36 % longer.
 #include "cache.h"
 
 namespace sale {
