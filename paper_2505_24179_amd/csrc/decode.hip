@@ -807,11 +807,11 @@ __global__ __launch_bounds__(512 * HALVES) void join_kernel(DecodeArgs a, int pr
     const int here = min(kMostWeights, parts - i0);
     if (i0 > 0) __syncthreads();
     for (int i = seat; i < (here + 7 & ~7); i += kSeats) {
-      const float2 x = i < here ? sum_of(i0 + i) : make_float2(0.0f, 0.0f);
-      // (a part without keys for this row has no accumulators)
-      const float w = x.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(x.x - top);
+      const float2 x = i < here ? sum_of(i0 + i) : make_float2(kNoRef, 0.0f);
+      // (a part without keys for this row: sum and accumulators are 0)
+      const float w = __builtin_amdgcn_exp2f(x.x - top);
       weight[i][n] = w;
-      if (x.y != 0.0f) l += w * x.y;
+      l += w * x.y;
     }
     __syncthreads();
     for (int i = half; i < here; i += 4 * HALVES) {
@@ -825,9 +825,11 @@ __global__ __launch_bounds__(512 * HALVES) void join_kernel(DecodeArgs a, int pr
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
+        // (By the part's number, not by its weight: what is not finite stays so under a weight that is too small for a float, as it does
+        // under the exponentials inside a part.)
         const float w = weight[i + HALVES * e][n];
 #pragma unroll
-        for (int f = 0; f < 4; ++f) acc[f] += w == 0.0f ? 0.0f : w * x[e][f];
+        for (int f = 0; f < 4; ++f) acc[f] += i + HALVES * e < here ? w * x[e][f] : 0.0f;
       }
     }
   }

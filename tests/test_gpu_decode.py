@@ -299,3 +299,29 @@ def test_what_the_binding_refuses(sale):
                  (k.transpose(2, 3), v.transpose(2, 3), t, n), (bits(k).view(torch.float8_e4m3fn)[..., :128], bits(v).view(torch.float8_e4m3fn)[..., :128], t, n)):
         with pytest.raises(ValueError):
             sale.Cache(*args)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("batch,prefix_len,top_in,bad_in", [(1, 0, "own", "own"), (1, 700, "prefix", "own"), (1, 700, "own", "prefix"), (20, 1100, "own", "prefix"),
+                                                            (20, 1100, "prefix", "own"), (1, 1100, "prefix", "prefix")])
+def test_a_bad_value_that_is_seen_is_not_lost_in_the_join(sale, kind, batch, prefix_len, top_in, bad_in):
+    """A NaN in V reaches every query that sees its key, also where another part of the keys has scores so much higher (by 500 and
+    more) that its weight is zero in fp32; so does an infinity, as one or as zero times infinity."""
+    gen = torch.Generator().manual_seed(17)
+    cache, prefix = make_cache(sale, [3000] + [1500] * (batch - 1), 1, 16, kind, "bhnd", gen, prefix_len, spoil=False)
+    cache.k.copy_(torch.zeros(cache.k.shape, dtype=torch.float32))
+    if kind == "fp8":
+        cache.k_scale.fill_(1.0)
+    place = {"own": lambda pos: (int(cache.table[0, pos // 16]), 0, pos % 16), "prefix": lambda pos: (int(prefix[pos // 16]), 0, pos % 16)}
+    value = torch.tensor(448.0).to(cache.k.dtype).cuda()
+    bits(cache.k)[place[top_in](690) + (0,)] = bits(value)
+    q = torch.zeros(batch, 4, 1, 128, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 16.0
+    for value in ("nan",) + (("inf",) if kind == "bf16" else ()):
+        bits(cache.v)[place[bad_in](5) + (slice(0, 128, 3),)] = bits(torch.tensor(float(value)).to(cache.v.dtype).cuda())
+        o, lse = sale.decode_attn(sale.Params(batch, 4, 1, 1), cache, q, prefix=prefix, prefix_len=prefix_len, want_lse=True)
+        assert not torch.isfinite(o[0, :, :, ::3]).any()
+        keep = [c for c in range(128) if value == "nan" or c % 3]
+        part = sale.Cache(cache.k, cache.v, cache.table[:1].contiguous(), cache.lens[:1].contiguous(), cache.k_scale, cache.v_scale)
+        want = decode_oracle(part, q[:1], prefix, prefix_len)
+        check(o[:1, ..., keep], lse[:1], [x[..., keep] if x.ndim == 4 else x for x in want])
