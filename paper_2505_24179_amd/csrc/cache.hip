@@ -69,13 +69,14 @@ struct AppendJob {
 // e4m3(x / scale), nearest, ties to even; at most 448 in size; NaN stays.  The quotient is the correctly rounded one: with
 // inv = 1 / scale correctly rounded, q = x inv is next to it and one step of Newton's with the exact remainder gives it (Markstein,
 // 1990), in 3 instructions where the compiler's division takes 10.  (q is limited first: from an infinite one the step would make a
-// NaN; what is limited there is limited in the end.)  A scale so far out that remainders could leave the range of a float takes
-// the division.
+// NaN; what is limited there is limited in the end.  The remainder is taken as q scale - x and subtracted: where it is zero it is
+// +0, and -0 - 0 is -0, so that zero keeps its sign, which x - q scale, added, would not.)  A scale so far out that remainders could
+// leave the range of a float takes the division.
 struct Divisor { float scale, inv; bool far; };
 __device__ __forceinline__ Divisor divisor(float scale) { return {scale, 1.0f / scale, !(scale >= 0x1p-60f && scale <= 0x1p60f)}; }
 __device__ __forceinline__ float quotient448(float x, const Divisor& d) {
   float q = __builtin_amdgcn_fmed3f(x * d.inv, -1000.0f, 1000.0f);
-  q = __builtin_fmaf(__builtin_fmaf(-q, d.scale, x), d.inv, q);
+  q = __builtin_fmaf(-__builtin_fmaf(q, d.scale, -x), d.inv, q);
   if (__builtin_expect(d.far, 0)) q = x / d.scale;
   return __builtin_elementwise_minimum(__builtin_elementwise_maximum(q, -448.0f), 448.0f);      // (a NaN passes these)
 }

@@ -142,3 +142,22 @@ def test_what_the_binding_refuses(sale):
     for src, dst in (([0], [0]), ([0, 1], [2, 2]), ([0], [99]), ([-1], [1])):
         with pytest.raises(sale.SaleError):
             sale.cache_copy(p, cache, src, dst)
+
+
+@pytest.mark.parametrize("page", [16, 64])
+def test_zero_keeps_its_sign_in_8_bits(sale, page):
+    """The codes of zeros and of what rounds to zero, as bits: those of IEEE division and rounding."""
+    gen = torch.Generator().manual_seed(8)
+    cache, _ = make_cache(sale, [4], 2, page, "fp8", "bhnd", gen)
+    cache.k_scale.copy_(torch.tensor([0.011, 3.0]))
+    cache.v_scale.copy_(torch.tensor([1e-25, 1e25]))      # (beyond the range of the quick quotient)
+    x = torch.zeros(1, 2, 4, 128, dtype=torch.bfloat16)
+    x[..., 0, 1::2] = -0.0
+    x[..., 1, :] = torch.tensor([-1e-40, 1e-40] * 64)
+    x[..., 2, :] = torch.linspace(-1e-4, 1e-4, 128)
+    x[..., 3, :] = torch.tensor([-0.0, -1.0] * 64)
+    want = [_expected(cache, x[0].transpose(0, 1), side, [4]) for side in ("k", "v")]
+    sale.cache_append(sale.Params(1, 4, 2, 4), cache, x.cuda(), x.cuda())
+    for side, w in zip(("k", "v"), want):
+        assert torch.equal(bits(getattr(cache, side)).cpu(), w), side
+    assert int((want[0] == 128).sum()) > 64
