@@ -1570,7 +1570,7 @@ void for_sequences_from_last(const sale_params_t* p, F f) {
 }
 PromptShape prompt_shape(const sale_params_t* p) {
   PromptShape s = {0, 0, 0, false};
-  auto blocks_of = [](int a, int z) { return (z - a + kBlockQ - 1) / kBlockQ; };
+  auto blocks_of = [](int a, int z) { return (int)(((long long)z - a + kBlockQ - 1) / kBlockQ); };
   long long work = 0;
   for_sequences_from_last(p, [&](int a, int z) {
     const int n = blocks_of(a, z);

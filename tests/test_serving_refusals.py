@@ -158,3 +158,12 @@ def test_the_binding_takes_device_tensors_only(sale):
         sale.Cache(k, k, torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32))
     with pytest.raises(ValueError, match="device tensor"):
         sale.prompt_attn(sale.Params(1, 2, 2, 5), *(torch.zeros(1, 2, 5, 128, dtype=torch.bfloat16) for _ in range(3)))
+
+
+def test_prompts_of_nearly_2_31_tokens(sale):
+    """Longer than any that is taken, also where their length and a block's would leave 32 bits together."""
+    lib, b = sale.raw(), ctypes.byref
+    for n in ((1 << 31) - 1, (1 << 31) - 63, (1 << 31) - 64, 1 << 30):
+        for kw in (dict(batch=1, n=n), dict(batch=1, hq=1, hkv=1, n=n), dict(batch=1, n=n, cu_seqlens=(0, n)), dict(batch=1, n=n, cu_seqlens=(0, 0, n, n))):
+            assert lib.sale_workspace_bytes(b(_params(sale, **kw)), sale.WS_PROMPT_ATTN) == 0
+            assert lib.sale_prompt_attn(b(_params(sale, **kw)), F, F, F, F, None, F, (1 << 64) - 1, None) == -3
