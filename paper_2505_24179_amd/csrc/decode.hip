@@ -919,7 +919,8 @@ Plan make_plan(const sale_params_t* p, const sale_cache_t* c, int prefix_len) {
   return w;
 }
 
-int validate_decode(const sale_params_t* p, const sale_cache_t* c, int prefix_len) {
+// What sale.h promises, and the plan.
+int plan_of(const sale_params_t* p, const sale_cache_t* c, int prefix_len, Plan& w) {
   int rc = validate_tokens(p);
   if (rc == SALE_OK) rc = validate_cache(p, c, true);
   if (rc != SALE_OK) return rc;
@@ -929,6 +930,10 @@ int validate_decode(const sale_params_t* p, const sale_cache_t* c, int prefix_le
   // (workgroups, rows and turns are counted in 32 bits)
   if (((long long)c->table_width * c->page_tokens / kTurn + 1) * p->batch > 0x7FFFFFFF) return SALE_ERR_UNSUPPORTED;
   if ((long long)p->batch * p->n_q_heads * p->seq_len > 0x3FFFFFFF || (long long)p->batch * p->n_kv_heads > (0x7FFFFFFF >> 8)) return SALE_ERR_UNSUPPORTED;
+  w = make_plan(p, c, prefix_len);
+  // (the join has 16 rows per workgroup, of 512 threads where there are many; the prefix 64 per workgroup of 256)
+  const long long join = (long long)p->batch * p->n_kv_heads * ((p->n_q_heads / p->n_kv_heads * p->seq_len + 15) / 16);
+  if ((!w.whole && 2 * join > kMostWorkgroups) || w.pre_slots > (size_t)kMostWorkgroups) return SALE_ERR_UNSUPPORTED;
   return SALE_OK;
 }
 
@@ -964,17 +969,17 @@ void launch_decode(const DecodeArgs& a, const Plan& w, hipStream_t st) {
 using namespace sale;
 
 extern "C" size_t sale_decode_workspace_bytes(const sale_params_t* p, const sale_cache_t* cache, int32_t prefix_len) {
-  if (!p || !cache || validate_decode(p, cache, prefix_len) != SALE_OK) return 0;
-  return make_plan(p, cache, prefix_len).bytes;
+  Plan w;
+  return p && cache && plan_of(p, cache, prefix_len, w) == SALE_OK ? w.bytes : 0;
 }
 
 extern "C" int sale_decode_attn(const sale_params_t* p, const sale_cache_t* cache, const void* q, const int32_t* prefix_table,
                                 int32_t prefix_len, void* o, float* lse, void* ws, size_t ws_bytes, void* stream) {
   if (!p || !cache || !q || !o || (prefix_len > 0 && !prefix_table)) return SALE_ERR_NULL_ARG;
-  const int rc = validate_decode(p, cache, prefix_len);
+  Plan w;
+  const int rc = plan_of(p, cache, prefix_len, w);
   if (rc != SALE_OK) return rc;
   if (((uintptr_t)q | (uintptr_t)o) & 15) return SALE_ERR_BAD_SHAPE;
-  const Plan w = make_plan(p, cache, prefix_len);
   if (w.bytes > 0 && (!ws || ws_bytes < w.bytes || ((uintptr_t)ws & 15))) return SALE_ERR_WORKSPACE;
   DecodeArgs a = {};
   a.c = cache_view(p, cache);

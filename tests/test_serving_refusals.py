@@ -167,3 +167,22 @@ def test_prompts_of_nearly_2_31_tokens(sale):
         for kw in (dict(batch=1, n=n), dict(batch=1, hq=1, hkv=1, n=n), dict(batch=1, n=n, cu_seqlens=(0, n)), dict(batch=1, n=n, cu_seqlens=(0, 0, n, n))):
             assert lib.sale_workspace_bytes(b(_params(sale, **kw)), sale.WS_PROMPT_ATTN) == 0
             assert lib.sale_prompt_attn(b(_params(sale, **kw)), F, F, F, F, None, F, (1 << 64) - 1, None) == -3
+
+
+def test_joins_of_too_many_threads(sale):
+    """More than 16 rows per KV head are joined 16 at a time, by workgroups of 512 threads: fewer than 2^32 of these too."""
+    lib, b = sale.raw(), ctypes.byref
+    c = _cache(sale, table_width=100)
+    size = lambda prefix=0, **kw: lib.sale_decode_workspace_bytes(b(_params(sale, **kw)), b(c), prefix)
+    call = lambda prefix=0, **kw: lib.sale_decode_attn(b(_params(sale, **kw)), b(c), F, F, prefix, F, None, F, 1 << 62, None)
+    for kw in (dict(batch=(1 << 22) + 1, hq=17, hkv=1), dict(batch=1 << 22, hq=17, hkv=1), dict(batch=1 << 21, hq=49, hkv=1), dict(batch=1 << 20, hq=8, hkv=4, n=25),
+               dict(batch=1 << 22, hq=1, hkv=1, n=33)):
+        assert size(**kw) == 0 and call(**kw) == -3
+        assert size(prefix=5, **kw) == 0 and call(prefix=5, **kw) == -3
+    # (smaller by a sequence: taken)
+    for kw in (dict(batch=(1 << 22) - 1, hq=17, hkv=1), dict(batch=(1 << 21) - 1, hq=49, hkv=1), dict(batch=(1 << 23) - 1, hq=1, hkv=1)):
+        assert size(**kw) > 0
+    # (left whole: there is no join)
+    c = _cache(sale, table_width=4)
+    assert lib.sale_decode_attn(b(_params(sale, batch=1 << 22, hq=17, hkv=1)), b(c), ctypes.c_void_p(0x1004), None, 0, F, None, None, 0, None) == -2
+    assert call(prefix=5, batch=1 << 22, hq=17, hkv=1) == -3
