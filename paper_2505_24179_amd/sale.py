@@ -545,11 +545,29 @@ def cache_copy(p: Params, cache: Cache, src, dst) -> None:
     _check(_lib.sale_cache_copy(p._contiguous, c, _ptr(src), _ptr(dst), src.numel(), _stream()))
 
 
-def decode_workspace_bytes(p: Params, cache: Cache, prefix_len: int = 0) -> int:
+_MOST_KEPT_SIZES = 256
+
+
+def _decode_size(p: Params, cache: Cache, prefix_len: int):
+    """-> bytes of workspace, and what to keep them by if they are not kept yet.  (The library says 0 of a cache that it refuses,
+    too, while another of these sizes may be a good one: 0 is kept once a call without a workspace has gone through.)"""
     key = (*cache._struct[5], prefix_len)
     n = p._ws_bytes.get(key)
-    if n is None:
-        n = p._ws_bytes[key] = int(_lib.sale_decode_workspace_bytes(p._contiguous, cache._arg(p, _n_sequences(p)), prefix_len))
+    if n is not None:
+        return n, None
+    return int(_lib.sale_decode_workspace_bytes(p._contiguous, cache._arg(p, _n_sequences(p)), prefix_len)), key
+
+
+def _keep_size(p: Params, key, n: int) -> None:
+    if len(p._ws_bytes) >= _MOST_KEPT_SIZES:      # (a program may go through any number of prefix lengths)
+        p._ws_bytes.clear()
+    p._ws_bytes[key] = n
+
+
+def decode_workspace_bytes(p: Params, cache: Cache, prefix_len: int = 0) -> int:
+    n, key = _decode_size(p, cache, prefix_len)
+    if n and key is not None:
+        _keep_size(p, key, n)
     return n
 
 
@@ -567,12 +585,15 @@ def decode_attn(p: Params, cache: Cache, q, prefix=None, prefix_len: int = 0, wa
     else:
         prefix = None
     lse = torch.empty(p.batch, p.n_q_heads, p.seq_len, dtype=torch.float32, device=q.device) if want_lse else None
+    key = None
     if ws is None:
-        n_ws = decode_workspace_bytes(p, cache, prefix_len)
+        n_ws, key = _decode_size(p, cache, prefix_len)
         if n_ws:
             ws = torch.empty(n_ws, dtype=torch.uint8, device=q.device)
     else:
         n_ws = _expect_ws(ws)
     _on_current_device("q prefix out workspace", q, prefix, o, ws)
     _check(_lib.sale_decode_attn(args, c, _ptr(q), _ptr(prefix), prefix_len, _ptr(o), _ptr(lse), _ptr(ws), n_ws, _stream()))
+    if key is not None:
+        _keep_size(p, key, n_ws)
     return o, lse

@@ -325,3 +325,24 @@ def test_a_bad_value_that_is_seen_is_not_lost_in_the_join(sale, kind, batch, pre
         part = sale.Cache(cache.k, cache.v, cache.table[:1].contiguous(), cache.lens[:1].contiguous(), cache.k_scale, cache.v_scale)
         want = decode_oracle(part, q[:1], prefix, prefix_len)
         check(o[:1, ..., keep], lse[:1], [x[..., keep] if x.ndim == 4 else x for x in want])
+
+
+def test_a_refused_cache_does_not_spoil_the_parameters(sale):
+    """The workspace of a cache that the library refuses is 0 bytes; a good one under the same parameters has its own."""
+    gen = torch.Generator().manual_seed(20)
+    cache, _ = make_cache(sale, [900, 2000], 2, 16, "bf16", "bhnd", gen, spoil=False)
+    p, q = sale.Params(2, 8, 2, 1), rows((2, 8, 1, 128), "bhnd", gen)
+    apart = torch.zeros(cache.k.shape[0], 2, 16, 132, dtype=torch.bfloat16, device="cuda")[..., :128]      # (no multiple of 16 bytes)
+    with pytest.raises(sale.SaleError):
+        sale.decode_attn(p, sale.Cache(apart, apart, cache.table, cache.lens), q)
+    o, lse = sale.decode_attn(p, cache, q, want_lse=True)
+    check(o, lse, decode_oracle(cache, q, None, 0))
+    short = sale.Cache(cache.k, cache.v, cache.table[:, :4].contiguous(), cache.lens)      # (left whole: no workspace)
+    for c in (sale.Cache(apart, apart, short.table, short.lens), short):
+        if c is short:
+            o, lse = sale.decode_attn(p, c, q, want_lse=True)
+            check(o, lse, decode_oracle(c, q, None, 0))
+        else:
+            with pytest.raises(sale.SaleError):
+                sale.decode_attn(p, c, q)
+        assert (0 in p._ws_bytes.values()) == (c is short)

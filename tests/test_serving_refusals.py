@@ -186,3 +186,34 @@ def test_joins_of_too_many_threads(sale):
     c = _cache(sale, table_width=4)
     assert lib.sale_decode_attn(b(_params(sale, batch=1 << 22, hq=17, hkv=1)), b(c), ctypes.c_void_p(0x1004), None, 0, F, None, None, 0, None) == -2
     assert call(prefix=5, batch=1 << 22, hq=17, hkv=1) == -3
+
+
+class _Given:
+    """What decode_workspace_bytes reads of a cache, without its tensors."""
+
+    def __init__(self, c, kind="bf16"):
+        self._struct, self._c = (c, 2, 128, 2, 0, (kind, c.page_tokens, c.table_width)), c
+
+    def _arg(self, p, sequences=None):
+        return self._c
+
+
+def test_the_size_of_a_refused_cache_is_not_kept(sale):
+    """Parameters keep the sizes that the library said for them; the 0 bytes of a cache that it refuses are none."""
+    good = _cache(sale, table_width=100)
+    need = sale.decode_workspace_bytes(sale.Params(2, 8, 2, 1), _Given(good))
+    assert need > 0
+    for bad in (_cache(sale, table_width=100, k_stride=(4224, 2112, 132)), _cache(sale, table_width=100, k=0x1008)):
+        p = sale.Params(2, 8, 2, 1)
+        assert sale.decode_workspace_bytes(p, _Given(bad)) == 0
+        assert sale.decode_workspace_bytes(p, _Given(good)) == need
+    assert sale.decode_workspace_bytes(p, _Given(_cache(sale, table_width=4))) == 0      # (needs none)
+
+
+def test_parameters_keep_few_sizes(sale):
+    """However many lengths of a prefix a program goes through."""
+    p, c = sale.Params(2, 8, 2, 1), _Given(_cache(sale, table_width=100))
+    attn = sale.workspace_bytes(p, sale.WS_PROMPT_ATTN)
+    sizes = [sale.decode_workspace_bytes(p, c, n) for n in range(1, 3000)]
+    assert len(p._ws_bytes) <= 300
+    assert sale.workspace_bytes(p, sale.WS_PROMPT_ATTN) == attn and [sale.decode_workspace_bytes(p, c, n) for n in (1, 130, 2999)] == [sizes[i] for i in (0, 129, 2998)]
