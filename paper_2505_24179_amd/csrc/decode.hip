@@ -337,9 +337,10 @@ __device__ __forceinline__ void sweep(const CacheView& c, const Keys& ks, int kv
 // the operand that the key becomes.  (128 sequences behind 32749 keys: operands straight from memory 100 us, this way 83.  Keys of
 // 8 bits are half the loads, and conversions take the time: 31.2 straight, 31.9 this way.)
 struct KeyBuffer { u32x4 of[kWaves][512]; };      // the keys of a step of every wave
-template <bool FP8, bool ONE>
+struct KeyBuffers { KeyBuffer even, odd; };
+template <bool FP8, bool ONE, class Lds>
 __device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int kvh, int key0, int steps, int lane, int wave, float scale,
-                                         KeyBuffer& even, KeyBuffer& odd, Rows<FP8, 4>& rows) {
+                                         Lds& lds, Rows<FP8, 4>& rows) {
   constexpr int NT = 4, kQk = 8 * NT, kPv = 8 * NT, kElems = 8 * NT, kLoads = FP8 ? 2 : 4;
   const int mask = (1 << c.page_shift) - 1;
   const LaneOffsets lane_at = lane_offsets<FP8>(c, lane);
@@ -374,11 +375,11 @@ __device__ __forceinline__ void pipeline(const CacheView& c, const Keys& ks, int
   auto get_k = [&](auto parity, const Tiles& from, int t, int s) __attribute__((always_inline)) {
     constexpr int p = decltype(parity)::value;
     if constexpr (FP8) load_k<FP8>(x[p], t, s, t == 0 ? from.a : from.b, lane_at.k, t * k_second);
-    else __builtin_amdgcn_raw_ptr_buffer_load_lds(t == 0 ? from.a : from.b, (__attribute__((address_space(3))) void*)&(p ? odd : even).of[wave][256 * t + 64 * s],
+    else __builtin_amdgcn_raw_ptr_buffer_load_lds(t == 0 ? from.a : from.b, (__attribute__((address_space(3))) void*)&(p ? lds.keys.odd : lds.keys.even).of[wave][256 * t + 64 * s],
                                                   16, to_lane[s], t * k_second, 0, 0);
   };
   auto read_k = [&](auto parity, int t, int s) __attribute__((always_inline)) {
-    if constexpr (!FP8) x[0].k[t][s] = (decltype(parity)::value ? odd : even).of[wave][256 * t + from_lane[s]];
+    if constexpr (!FP8) x[0].k[t][s] = (decltype(parity)::value ? lds.keys.odd : lds.keys.even).of[wave][256 * t + from_lane[s]];
   };
   constexpr std::integral_constant<int, 0> in_even{};
   constexpr std::integral_constant<int, 1> in_odd{};
@@ -727,9 +728,13 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void own_kernel(Decod
 }
 
 // A workgroup: one part of the prefix, for 16 NT rows of one KV head, of whichever sequences.
+// (All LDS of the kernel is one object, of which the keys come first: a load's place there is documented as a number of 16 bits.)
+struct KeysAndJoin { KeyBuffers keys; JoinLds join; };
+struct JoinAlone { JoinLds join; };
+static_assert(sizeof(KeyBuffers) <= 65536, "the pipeline's keys lie below 64 KB of LDS");
 template <bool FP8, int NT>
 __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void prefix_kernel(DecodeArgs a) {
-  __shared__ JoinLds lds;
+  __shared__ __attribute__((aligned(1024))) std::conditional_t<NT == 4 && !FP8, KeysAndJoin, JoinAlone> lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, g = lane >> 4, n_rows = a.group * a.n_new;
   const int kvh = blockIdx.x % a.n_kvh, rest = blockIdx.x / a.n_kvh, tile = rest % a.row_tiles, part = rest / a.row_tiles;
@@ -751,15 +756,13 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void prefix_kernel(De
     for (int i = (lo >> a.c.page_shift) + lane; i <= (hi - 1) >> a.c.page_shift; i += 64) missing |= (unsigned)ks.table[i] >= (unsigned)a.c.n_pages;
     const int steps = (max(hi - from, 0) / kStep + kWaves - 1) / kWaves & ~1;
     if (steps > 0 && __builtin_amdgcn_ballot_w64(missing) == 0) {
-      // (Aligned so that they come first in LDS, below 64 KB: a load's place there is documented as a number of 16 bits.)
-      __shared__ __attribute__((aligned(1024))) KeyBuffer even, odd;
-      if (a.c.page_shift >= 5) pipeline<FP8, true>(a.c, ks, kvh, from, steps, lane, wave, scale, even, odd, rows);
-      else pipeline<FP8, false>(a.c, ks, kvh, from, steps, lane, wave, scale, even, odd, rows);
+      if (a.c.page_shift >= 5) pipeline<FP8, true>(a.c, ks, kvh, from, steps, lane, wave, scale, lds, rows);
+      else pipeline<FP8, false>(a.c, ks, kvh, from, steps, lane, wave, scale, lds, rows);
       from += steps * kTurn;
     }
   }
   sweep<FP8, NT, NT != 4>(a.c, ks, kvh, from, hi, lane, 1, scale, rows);
-  join_waves<FP8, NT>(rows, lds, wave, lane,
+  join_waves<FP8, NT>(rows, lds.join, wave, lane,
     [&](int qt, int c, f32x4 x, float) { a.pre_acc[((slot * 8 + c) * 4 + g) * (16 * NT) + 16 * qt + n] = x; },
     [&](int row, float ref, float l) { a.pre_sum[slot * 16 * NT + row] = make_float2(ref, l); });
 }

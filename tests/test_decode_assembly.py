@@ -108,3 +108,30 @@ def test_keys_in_lds_have_their_waits(kernels):
                 prologues += 1
                 assert re.match(r"K*L{16}w+(?:RK*){8}(?<=K)L{8}P{8}[wW]+(?:RK*){8}", events), (name, events)
     assert (phases, prologues) == (4, 2)
+
+
+def test_keys_lie_below_64_kb_of_lds(kernels):
+    """A load to LDS takes its place from m0, documented as 16 bits: 8 KB times the wave's number and a constant here."""
+    checked = 0
+    for name, body in kernels[1].items():
+        place = {}      # registers that hold 8 KB * wave and a constant
+        for line in body:
+            op, _, rest = line.split(";")[0].strip().partition(" ")
+            args = [x.strip() for x in rest.split(",")]
+            if op == "s_lshl_b32" and args[2] == "13":
+                at = 0
+            elif op in ("s_or_b32", "s_add_i32", "s_add_u32", "s_addk_i32") and args[-2] in place and re.fullmatch(r"0x[0-9a-f]+|\d+", args[-1]):
+                at = place[args[-2]] + int(args[-1], 0)
+            elif op == "s_mov_b32":
+                at = place.get(args[1])
+            else:
+                at = None
+            if op.startswith("s_"):
+                if args[0] == "m0":
+                    checked += 1
+                    assert at is not None and 3 * 8192 + at + 1024 <= 65536, (name, line)
+                for r in _registers(args[0], "s"):
+                    place.pop(f"s{r}", None)
+                if at is not None:
+                    place[args[0]] = at
+    assert checked == 2 * (16 + 8 + 16)      # a step in one page or two: before the loop 16 and 8, its two phases 8 each
