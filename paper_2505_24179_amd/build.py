@@ -5,6 +5,7 @@ Usage: python -m paper_2505_24179_amd.build
 from __future__ import annotations
 
 import os
+import re
 import subprocess
 import sys
 from concurrent.futures import ThreadPoolExecutor
@@ -25,13 +26,28 @@ FLAGS = [
 ]
 
 
+# Sources whose kernels may keep nothing in scratch memory: with matrix results in ordinary registers this compiler has made wrong
+# code of a kernel that used accumulation registers and spilled.
+NO_SCRATCH = ("decode.hip",)
+_REPORT = "-Rpass-analysis=kernel-resource-usage"
+
+
 def _compile(src: str, extra) -> str:
     obj = os.path.join(CSRC, src.replace(".hip", ".o"))
-    cmd = [HIPCC, *FLAGS, *extra, "-c", os.path.join(CSRC, src), "-o", obj]
+    report = [_REPORT, "-fno-caret-diagnostics"] if src in NO_SCRATCH else []
+    cmd = [HIPCC, *FLAGS, *report, *extra, "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
-    err = "\n".join(l for l in r.stderr.splitlines() if "packed-fp32-ops" not in l and l.strip())
+    remarks = [l for l in r.stderr.splitlines() if _REPORT in l]
+    err = "\n".join(l for l in r.stderr.splitlines() if "packed-fp32-ops" not in l and _REPORT not in l and l.strip())
     if r.returncode != 0:
         raise RuntimeError(f"hipcc failed for {src}:\n{err}")
+    if report:
+        sizes = [re.search(r"ScratchSize \[bytes/lane\]: (\w+)", l) for l in remarks]
+        sizes = [m[1] for m in sizes if m]
+        if not sizes or any(n != "0" for n in sizes):
+            os.remove(obj)
+            raise RuntimeError(f"{src}: kernels that keep values in scratch memory (bytes per lane: {', '.join(sizes) or 'not reported'}); this "
+                               "compiler or these flags may make wrong code of them")
     if err:
         print(err, file=sys.stderr)
     return obj
