@@ -346,3 +346,65 @@ def test_a_refused_cache_does_not_spoil_the_parameters(sale):
             with pytest.raises(sale.SaleError):
                 sale.decode_attn(p, c, q)
         assert (0 in p._ws_bytes.values()) == (c is short)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("hq,lens,prefix_len,room", [(1, [40001], 20000, 1), (4, [32000], 16384, 1), (4, [66000], 0, 13000), (1, [66000], 16300, 13000)])
+def test_more_parts_than_weights_at_a_time(sale, kind, hq, lens, prefix_len, room):
+    """One KV head and one sequence: 250 .. 512 pieces of own keys (8-bit pages: 512 where the table has room for much), 79 or 128 parts of the prefix."""
+    gen = torch.Generator().manual_seed(18)
+    cache, prefix = make_cache(sale, lens, 1, 16, kind, "bhnd", gen, prefix_len, room=room, spoil=False)
+    q = rows((1, hq, 1, 128), "bhnd", gen, 2.0)
+    o, lse = sale.decode_attn(sale.Params(1, hq, 1, 1), cache, q, prefix=prefix, prefix_len=prefix_len, want_lse=True)
+    check(o, lse, decode_oracle(cache, q, prefix, prefix_len))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("page", [16, 64])
+def test_a_query_that_is_not_finite_among_many_rows(sale, kind, page):
+    """64 rows and more of a long prefix: the others' results keep their bits."""
+    gen = torch.Generator().manual_seed(19)
+    batch, prefix_len = 40, 5000
+    cache, prefix = make_cache(sale, [5] * batch, 1, page, kind, "bhnd", gen, prefix_len)
+    p, q = sale.Params(batch, 4, 1, 1), rows((batch, 4, 1, 128), "bhnd", gen, 2.0)
+    clean, clean_lse = sale.decode_attn(p, cache, q, prefix=prefix, prefix_len=prefix_len, want_lse=True)
+    hit = torch.zeros(batch, 4, 1, dtype=torch.bool, device="cuda")
+    for s, h, value in ((0, 1, "nan"), (17, 2, "inf"), (18, 0, "-inf"), (39, 3, "nan")):
+        q[s, h, 0, 5], hit[s, h, 0] = float(value), True
+    o, lse = sale.decode_attn(p, cache, q, prefix=prefix, prefix_len=prefix_len, want_lse=True)
+    assert torch.isnan(o[hit]).all()
+    assert torch.equal(o[~hit], clean[~hit]) and torch.equal(lse[~hit], clean_lse[~hit])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("batch,n,prefix_len", [(3, 1, 0), (3, 6, 40), (33, 2, 2100)])
+def test_keys_and_values_of_different_layouts(sale, kind, batch, n, prefix_len):
+    gen = torch.Generator().manual_seed(21)
+    lens = [1000, 0, 77] * (batch // 3)
+    cache, prefix = make_cache(sale, lens, 2, 32, kind, "padded", gen, prefix_len)
+    v = bits(cache.v).transpose(1, 2).contiguous().transpose(1, 2).view(cache.v.dtype)
+    q = rows((batch, 8, n, 128), "bnhd", gen, 2.0)
+    p = sale.Params(batch, 8, 2, n)
+    for c in (sale.Cache(cache.k, v, cache.table, cache.lens, cache.k_scale, cache.v_scale),
+              sale.Cache(bits(cache.k).contiguous().view(cache.k.dtype), v, cache.table, cache.lens, cache.k_scale, cache.v_scale)):
+        o, lse = sale.decode_attn(p, c, q, prefix=prefix, prefix_len=prefix_len, want_lse=True)
+        _some(sale, c, q, o, lse, prefix, prefix_len, [0, 1, batch - 1])
+        assert torch.equal(o, sale.decode_attn(p, cache, q, prefix=prefix, prefix_len=prefix_len)[0])
+
+
+@pytest.mark.parametrize("n", [1, 5])
+@pytest.mark.parametrize("prefix_len", [0, 50])
+def test_a_batch_that_holds_nothing(sale, n, prefix_len):
+    """Under a table with room for much: every sequence empty; then one token in the last one."""
+    gen = torch.Generator().manual_seed(22)
+    cache, prefix = make_cache(sale, [0] * 9, 2, 16, "bf16", "bhnd", gen, prefix_len, room=300)
+    p, q = sale.Params(9, 8, 2, n), rows((9, 8, n, 128), "bhnd", gen)
+    for last in (0, 1):
+        if last:
+            cache.table[8, 0] = 0
+            cache.k[0], cache.v[0] = 1.0, 2.0
+            cache.lens[8] = 1
+        o, lse = sale.decode_attn(p, cache, q, prefix=prefix, prefix_len=prefix_len, want_lse=True)
+        check(o, lse, decode_oracle(cache, q, prefix, prefix_len))
+        if prefix_len == 0:
+            assert bool((o[:8] == 0).all() and (lse[:8] == -float("inf")).all())

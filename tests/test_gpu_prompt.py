@@ -166,3 +166,53 @@ def test_what_the_binding_refuses(sale):
         sale.prompt_attn(sale.Params(1, 4, 2, 50, flags=sale.FLAG_ATTN_INT8_QK), q, k, k)
     with pytest.raises(sale.SaleError):
         sale.prompt_attn(p, q, k, k, ws=torch.empty(100, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("offsets,hq,hkv", [((0, 2751), 32, 8), ((0, 1309, 1310, 3001), 32, 8)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_a_later_token_that_is_not_finite_in_a_large_call(sale, offsets, hq, hkv, value):
+    """As above, with more rows than two waves per row are taken for; in a sequence's last block, which is partly filled, too."""
+    gen = torch.Generator().manual_seed(15)
+    n, t0 = offsets[-1], offsets[-2]
+    q, k, v = (rows((1, h, n, 128), "bhnd", gen) for h in (hq, hkv, hkv))
+    p = sale.Params(1, hq, hkv, n, cu_seqlens=offsets if len(offsets) > 2 else ())
+    clean, clean_lse = sale.prompt_attn(p, q, k, v, want_lse=True)
+    for at in (t0 + 70, n - 9, n - 1):
+        k2, v2 = k.clone(), v.clone()
+        v2[:, :, at, ::5] = value
+        o, lse = sale.prompt_attn(p, q, k, v2, want_lse=True)
+        block = t0 + (at - t0) // 64 * 64
+        assert torch.equal(lse, clean_lse) and torch.equal(o[:, :, :block], clean[:, :, :block])
+        assert not torch.isfinite(o[:, :, at:, ::5]).any() and torch.isfinite(o[:, :, :at]).all()
+        some = sorted({block, at - 1, at, n - 1})
+        seen = np.arange(n - t0)[None] <= np.array(some)[:, None] - t0
+        keep = [c for c in range(128) if c % 5]
+        for h in (0, hq - 1):
+            want = so.attend(f64(q)[0, h, some], f64(k)[0, h * hkv // hq, t0:], f64(v)[0, h * hkv // hq, t0:], seen)
+            check(o[0, h, some][:, keep], None, [x[:, keep] if x.ndim == 2 else x for x in want])
+            before = [i for i, t in enumerate(some) if t < at]
+            check(o[0, h, some][before], None, [x[before] for x in want])
+        k2[:, :, at] = value
+        o, lse = sale.prompt_attn(p, q, k2, v2, want_lse=True)
+        assert torch.equal(o[:, :, :block], clean[:, :, :block]) and torch.equal(lse[:, :, :at], clean_lse[:, :, :at])
+        assert torch.isfinite(o[:, :, :at]).all()
+
+
+@pytest.mark.parametrize("n,hq,hkv", [(900, 2, 1), (2751, 32, 8)])
+def test_an_earlier_value_that_is_not_finite_is_not_lost(sale, n, hq, hkv):
+    """Behind it, scores so much higher that its probabilities are zero in fp32; and beside sequences that it is not part of."""
+    gen = torch.Generator().manual_seed(16)
+    q, k, v = (torch.zeros(1, h, n, 128, dtype=torch.bfloat16, device="cuda") for h in (hq, hkv, hkv))
+    q[..., 0] = 16.0
+    k[:, :, 50, 0] = 20.0
+    k[:, :, 600, 0] = 400.0
+    v.copy_(rows((1, hkv, n, 128), "bhnd", gen))
+    v[:, :, 3, ::7] = float("nan")
+    offsets = (0, 1, n - 130, n)
+    for offs in ((), offsets):
+        p = sale.Params(1, hq, hkv, n, cu_seqlens=offs)
+        o, _ = sale.prompt_attn(p, q, k, v)
+        end = n if not offs else n - 130
+        assert torch.isnan(o[:, :, 3:end, ::7]).all() and torch.isfinite(o[:, :, :3]).all() and torch.isfinite(o[:, :, end:]).all()
+        keep = [c for c in range(128) if c % 7]
+        assert torch.isfinite(o[..., keep]).all()
