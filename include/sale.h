@@ -416,15 +416,17 @@ int sale_cache_copy(const sale_params_t* p, const sale_cache_t* cache, const int
  * cache.  All sequences share a prefix of prefix_len keys, whose pages are prefix_table and which are read once for all
  * of them; a sequence's own keys, its new tokens among them (append first), follow it.  Query t of sequence s sees the
  * prefix and the own positions 0 .. lens[s] - seq_len + t.  O = softmax(Q K^T / sqrt(d)) V over these: sums of the
- * probabilities in fp32; the factors of V are the probabilities rounded to bf16, or better.  A query that sees no key (an
- * empty slot of the batch) gets O = 0 and lse = -inf.  Keys that a query does not see have no effect, whatever is in their
- * place.
+ * probabilities in fp32; the factors of V are the probabilities rounded to bf16, or better: to two bf16 each (16 bits) for the
+ * own keys where n_q_heads / n_kv_heads * seq_len is at most 16, for the prefix where that times batch is at most 32.  A query
+ * that sees no key (an empty slot of the batch) gets O = 0 and lse = -inf.  Keys that a query does not see have no effect,
+ * whatever is in their place; a NaN or an infinity in a value that it sees leaves that channel of its O not finite.
  *   p            : batch = sequences; n_q_heads / n_kv_heads * seq_len at most 64; n_seqs = 0
  *   q        in  : bf16, strided;  o out: bf16, strided
  *   prefix_table in : int32 [ceil(prefix_len / page_tokens)] (device), entries as in the table; NULL if prefix_len = 0
  *   lse      out : optional fp32 [batch][n_q_heads][seq_len], natural log of the sum
  *   ws           : workspace of sale_decode_workspace_bytes(p, cache, prefix_len) bytes (0: none needed)
- * The workspace and the launches follow from the sizes given here, not from lens: a captured call serves every lens.  Which
+ * The workspace and the launches follow from the sizes given here, table_width among them, not from lens: a captured call
+ * serves every lens, and short sequences are faster under a table that has room for little more than they hold.  Which
  * workgroup has which keys follows from all lens, so the last bits of a sequence's results may depend on the lengths of the
  * others; the same arguments give the same bits.
  */

@@ -135,7 +135,7 @@ class Cache:
     k, v             [pages, KV heads, tokens of a page, head_dim], torch.bfloat16 or torch.float8_e4m3fn, of any strides whose
                      last dimension is contiguous
     table            int32 [sequences, width]: the pages of each sequence in order, -1 (or anything that is no page) where
-                     there is none
+                     there is none (decode_attn's launches and workspace go by the width: no wider than needed is faster)
     lens             int32 [sequences]: tokens that each sequence holds
     k_scale, v_scale fp32 [KV heads], 8-bit pages only: a key is value * k_scale
 
