@@ -368,7 +368,8 @@ int sale_prompt_attn(const sale_params_t* p, const void* q, const void* k, const
  * belongs to whom; the calls read the structure itself during the call and everything it points to on the stream.
  *   element (page, KV head h, token slot, c) of K lies at  k + page * k_stride[0] + h * k_stride[1] + slot * k_stride[2] + c
  * (all-zero strides: contiguous [page][n_kv_heads][page_tokens][head_dim]); strides are non-negative multiples of 16 bytes,
- * the token stride head_dim .. 2^22 elements, the page stride less than 4 GB; V likewise.
+ * the token stride head_dim .. 2^22 elements, the page stride less than 4 GB; V likewise.  Where the calls write, no two
+ * elements of the pages of K and V lie in the same place.
  *   table : int32 [sequences][table_width], the pages of each sequence in order: position i of sequence s is slot
  *           i % page_tokens of page table[s][i / page_tokens].  An entry outside 0 .. n_pages - 1 is no page: its positions
  *           hold no keys and what is appended there is dropped.

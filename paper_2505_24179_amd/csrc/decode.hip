@@ -868,7 +868,7 @@ __global__ __launch_bounds__(512 * HALVES) void join_kernel(DecodeArgs a, int pr
 // of 32000 31.0, 35.2, 40.9; 16 of 500 .. 1000 19.9, 19.0, 20.2; 128 of 1000 .. 2000 150, 150, 160.  8-bit pages have half the bytes
 // in flight per workgroup and want two per CU where there is much to read: 128 of 1000 .. 2000 93.9, 83.0, 98.3; 16 of 4000 .. 8000
 // 47.5, 43.5, 47.3; but one of 8000 15.1, 18.3; one of 32000 23.6, 26.3.  So do short sequences (here behind a prefix), whose pieces
-// each begin with a wait that another workgroup can fill (kShortTurns): kernel, 256, 512, 768 workgroups, 128 of 0 .. 300 keys 24.1, 17.6, 19.9;
+// each begin with a wait that another workgroup can fill: kernel, 256, 512, 768 workgroups, 128 of 0 .. 300 keys 24.1, 17.6, 19.9;
 // 0 .. 1000 48.4, 44.8, 44.1, four new tokens each 54.6, 47.1, 46.2; 32 of 0 .. 1000 17.5, 15.6, 15.1; but 0 .. 2000 101, 102, 102, and 0 .. 4000
 // 188, 193, 189.
 // The parts of the prefix likewise, of either type, for up to 32 rows: 4 sequences behind 32000 keys 37.9, 42.2, 49.4, on 8-bit pages
@@ -878,11 +878,12 @@ __global__ __launch_bounds__(512 * HALVES) void join_kernel(DecodeArgs a, int pr
 // pages 38.9, 69.8, 55.6, 93.9, 107, 88.1, 156, 194.
 // (Cut into a number of parts that each sequence had to itself, the 64 took 251: the parts of the longest ended last.)
 constexpr int kCus = 256, kPlentyTurns = 2048, kShortTurns = 12;
-// Without a prefix, short sequences are left whole: one launch, and nothing to join.  (Short: what their tables have room for.  The
-// launches may not depend on lens, so a wide table of short sequences is cut like long ones: call, one sequence of 531 keys 11.2, with
-// room for 32K or 128K tokens 14.1; 16 of them 12.4, 17.1; 128 of 0 .. 1000 48.5, 52.5; these behind 32749 keys 143.6, 144.7.)  us, cut -> whole, 8 KV heads: one sequence of
+// Without a prefix, short sequences are left whole: one launch, and nothing to join.  us, cut -> whole, 8 KV heads: one sequence of
 // 531 keys 14.9 -> 11.0, 750 15.0 -> 12.7, 1000 14.8 -> 15.5; 16 x 531 16.7 -> 12.5; 32 x 0 .. 1000 22.8 -> 18.9, 0 .. 1300 24.8 ->
 // 22.6; 128 x 0 .. 1300 75.6 -> 72.9.
+// Short, here and above, is what the tables have room for: the launches may not depend on lens, so that a wide table of short sequences
+// is cut like that of long ones.  Call, under a table as wide as the keys -> one for 32K or 128K tokens: one sequence of 531 keys
+// 11.2 -> 14.1, 16 of them 12.4 -> 17.1; 128 of 0 .. 1000 48.5 -> 52.5, behind 32749 keys 143.6 -> 144.7.
 constexpr int kWholeTurns = 6, kManyUnits = 256, kWholeTurnsOfMany = 10;
 struct Plan {
   int own_tiles, pre_tiles;      // 16-row tiles per workgroup

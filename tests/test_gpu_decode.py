@@ -408,3 +408,35 @@ def test_a_batch_that_holds_nothing(sale, n, prefix_len):
         check(o, lse, decode_oracle(cache, q, prefix, prefix_len))
         if prefix_len == 0:
             assert bool((o[:8] == 0).all() and (lse[:8] == -float("inf")).all())
+
+
+def _bound_by_largest(o, slack, most):
+    """As the oracle's, with the largest |v| in the place of the average."""
+    return 2.0 ** -8 * (2 * np.abs(o) + most) + 2 * slack[..., None] * most
+
+
+@pytest.mark.parametrize("batch,n,prefix_len,at", [(1, 1, 0, "own"), (3, 1, 1100, "prefix"), (3, 1, 1100, "own"), (20, 1, 1100, "prefix"), (20, 1, 1100, "own"), (3, 6, 300, "prefix")])
+@pytest.mark.parametrize("value", ["nan", "inf", "-inf"])
+def test_a_key_that_is_seen_and_not_finite(sale, batch, n, prefix_len, at, value):
+    """A score of NaN or infinity makes O and lse NaN; one of minus infinity has no weight."""
+    gen = torch.Generator().manual_seed(23)
+    cache, prefix = make_cache(sale, [1500] + [40] * (batch - 1), 1, 16, "bf16", "bhnd", gen, prefix_len, spoil=False)
+    pos = min(200, prefix_len - 1) if at == "prefix" else 700
+    cache.k[int(prefix[pos // 16]) if at == "prefix" else int(cache.table[0, pos // 16]), 0, pos % 16, 5] = float(value)
+    q = rows((batch, 4, n, 128), "bhnd", gen, 2.0)
+    q[:, :2, :, 5], q[:, 2:, :, 5] = 1.5, -1.5
+    o, lse = sale.decode_attn(sale.Params(batch, 4, 1, n), cache, q, prefix=prefix, prefix_len=prefix_len, want_lse=True)
+    part = sale.Cache(cache.k, cache.v, cache.table[:1].contiguous(), cache.lens[:1].contiguous())
+    want = decode_oracle(part, q[:1], prefix, prefix_len)
+    lost = np.isnan(want[0][0, :, 0, 0])
+    assert lost.tolist() == {"nan": [True] * 4, "inf": [True, True, False, False], "-inf": [False, False, True, True]}[value]
+    assert torch.isnan(o[0, lost]).all() and torch.isnan(lse[0, lost]).all()
+    sound = ~lost
+    if sound.any():
+        # (the bound without the key itself, whose size is infinite)
+        cache.k[int(prefix[pos // 16]) if at == "prefix" else int(cache.table[0, pos // 16]), 0, pos % 16, 5] = 0.0
+        slack = decode_oracle(part, q[:1], prefix, prefix_len)[3]
+        tol = _bound_by_largest(want[0], slack, f64(cache.v).__abs__().max())
+        got = f64(o[:1])[:, sound]
+        assert (np.abs(got - want[0][:, sound]) <= tol[:, sound]).all()
+        assert (np.abs(f64(lse[:1])[:, sound] - want[1][:, sound]) <= slack[:, sound] + np.abs(want[1][:, sound]) * 2.0 ** -22 + 2.0 ** -20).all()
