@@ -10,6 +10,7 @@ import ctypes
 import os
 from dataclasses import dataclass, fields
 from functools import cached_property
+from operator import index
 
 import torch
 
@@ -529,7 +530,10 @@ def cache_append(p: Params, cache: Cache, k, v) -> None:
 
 def _host_pages(name: str, pages):
     if not isinstance(pages, torch.Tensor):
-        pages = torch.tensor(pages, dtype=torch.int32)
+        try:
+            pages = torch.tensor([index(x) for x in pages], dtype=torch.int32)      # (a float would be rounded without a word)
+        except (TypeError, RuntimeError) as e:
+            raise ValueError(f"{name}: expected a list of pages, whole numbers of 32 bits") from e
     if pages.is_cuda or pages.dtype != torch.int32 or pages.dim() != 1 or not pages.is_contiguous():
         raise ValueError(f"{name}: expected a list of pages, or a contiguous one-dimensional int32 tensor on the host")
     return pages

@@ -217,3 +217,17 @@ def test_parameters_keep_few_sizes(sale):
     sizes = [sale.decode_workspace_bytes(p, c, n) for n in range(1, 3000)]
     assert len(p._ws_bytes) <= 300
     assert sale.workspace_bytes(p, sale.WS_PROMPT_ATTN) == attn and [sale.decode_workspace_bytes(p, c, n) for n in (1, 130, 2999)] == [sizes[i] for i in (0, 129, 2998)]
+
+
+@pytest.mark.parametrize("pages", [[1.7], [0, 2.0], torch.zeros(2), torch.zeros(2, dtype=torch.int64), torch.zeros(1, 2, dtype=torch.int32),
+                                   torch.zeros(4, dtype=torch.int32)[::2], [[1, 2]], [1 << 31], [-(1 << 31) - 1]])
+def test_pages_that_are_no_list_of_pages(sale, pages):
+    with pytest.raises(ValueError, match="src"):
+        sale._host_pages("src", pages)
+
+
+def test_lists_of_pages(sale):
+    import numpy as np
+    for pages in ([], [3, 1, (1 << 31) - 1], (5,), np.array([4, 2]), [np.int64(7)], torch.tensor([1, 2], dtype=torch.int32)):
+        got = sale._host_pages("src", pages)
+        assert got.dtype == torch.int32 and got.is_contiguous() and got.tolist() == [int(x) for x in pages]
