@@ -396,7 +396,7 @@ typedef struct sale_cache {
  * Writes the keys and values of new tokens into the cache.  With n the number of new tokens of sequence s (seq_len, or the
  * length of packed sequence s), token i of them goes to position lens[s] - n + i: lens already counts the new tokens.
  * Tokens whose position is negative, lies beyond the table or in no page are dropped.  Nothing else of the pages is
- * written.  Where two sequences of a call write the same slot of a page, one of the two values is left there.
+ * written.  Where two sequences of a call write the same slot of a page, each element left there is that of one of the two.
  *   k, v in : bf16, strided as everywhere.  SALE_PAGE_FP8 keeps e4m3(x / scale[h]): IEEE fp32 division, limited to +-448,
  *             round to nearest even, NaN stays NaN.
  */
